@@ -438,6 +438,116 @@ mbq_status mbq_routed_linear_group_act(const uint16_t* X, int64_t T, int64_t K, 
                                        float* row_scale, uint16_t* Xr, void* ws_route, size_t ws_route_bytes,
                                        void* ws_linear, size_t ws_linear_bytes, int algo, void* stream);
 
+/*
+ * Beside a frozen blob: low-rank adapters and the routers' training
+ * -------------------------------------------------------------------------------------------------------------
+ * An encoded matrix is not written again; what is served and trained next to it are low-rank adapters on the shared
+ * projections and the routers (Sec. 4.2; the paper trains its routers against a target precision, Eq. 7).
+ *
+ * Adapters.  A pool holds n_adapters of them at one rank r, both factors rank-major: A [n_adapters][r][K] and
+ * B [n_adapters][r][N], bf16.  Token t names its adapter a(t) (or none), whose product is added to the shared projection's
+ * row:
+ *   H[t][j] = sum_k X[t][k] A[a(t)][j][k]
+ *   Y[t][n] = base[t][n] + scale[a(t)] sum_j H[t][j] B[a(t)][j][n]
+ * with j below the adapter's own rank ranks[a] (r where ranks is NULL; values are clamped to 0 .. r); what the pool holds in
+ * rows beyond it is not used, whatever it is.  fp32 accumulate throughout.
+ *
+ * Tokens are handed over as the linear calls have them, but by adapter:
+ *   adapter : int32 [T], the token's adapter; a value outside 0 .. n_adapters-1 is none
+ *   perm    : int32 [T], token ids grouped by ascending adapter, those of none last (mbq_lora_sort: stable)
+ *   offsets : int32 [n_adapters + 1]: the tokens of adapter a are perm[offsets[a] .. offsets[a+1]-1]
+ * The three must be mutually consistent.
+ */
+#define MBQ_LORA_MAX_RANK 256
+#define MBQ_LORA_MAX_ADAPTERS 65536
+/* perm and offsets of an assignment.  T = 0 is legal (offsets are zero-filled). */
+mbq_status mbq_lora_sort(const int32_t* adapter, int64_t T, int64_t n_adapters, int32_t* perm, int32_t* offsets,
+                         void* stream);
+/*
+ * mbq_lora_group - the adapters of n_proj projections that read the SAME activations (q/k/v, gate/up, or one alone),
+ * each with its own pools, all with the same assignment, scales and ranks.
+ *   X      : bf16 [T][K], 16-byte aligned; K a multiple of 128
+ *   A_host, B_host, N_host : HOST arrays of n_proj: pools (A 16-byte aligned, B 2-byte; 1 <= r <= MBQ_LORA_MAX_RANK), widths
+ *   ranks  : int32 [n_adapters], or NULL;   scale : fp32 [n_adapters]
+ *   base_host : HOST array of n_proj fp32 [T][N_i], what the shared projections gave; the array or an entry may be NULL
+ *            (zero), an entry may be the Y of the same projection (added in place) but not overlap an output otherwise
+ *   Y_host : HOST array of n_proj fp32 [T][N_i], written for every token (those without an adapter: base)
+ *   H_host : HOST array of n_proj fp32 [T][r] (out, kept for the backward pass), or NULL; zero for tokens without an
+ *            adapter and beyond an adapter's rank
+ *   ws     : at least mbq_lora_workspace_bytes(T, K, n_proj, r) bytes, 256-byte aligned, contents do not matter
+ * The arrays are read before the call returns.  1 <= n_proj <= MBQ_MAX_GROUP.  T = 0 is legal (no-op).  Equal calls give
+ * equal bits.
+ */
+size_t mbq_lora_workspace_bytes(int64_t T, int64_t K, int n_proj, int r);
+mbq_status mbq_lora_group(const uint16_t* X, int64_t T, int64_t K, int n_proj, const uint16_t* const* A_host,
+                          const uint16_t* const* B_host, const int64_t* N_host, int64_t n_adapters, int r,
+                          const int32_t* ranks, const float* scale, const int32_t* adapter, const int32_t* perm,
+                          const int32_t* offsets, const float* const* base_host, float* const* Y_host,
+                          float* const* H_host, void* ws, size_t ws_bytes, void* stream);
+/*
+ * mbq_lora_backward_group - gradients of mbq_lora_group for the same X, pools and assignment.  With G_p[t][j] =
+ * scale[a(t)] sum_n dY_p[t][n] B_p[a(t)][j][n] (j below the adapter's rank):
+ *   dX[t][k]       = base[t][k] + sum_p sum_j G_p[t][j] A_p[a(t)][j][k]
+ *   dA_p[a][j][k]  = sum over the tokens of a of G_p[t][j] X[t][k]
+ *   dB_p[a][j][n]  = scale[a] sum over the tokens of a of H_p[t][j] dY_p[t][n]
+ *   dY_host : HOST array of n_proj fp32 [T][N_i];  H_host : HOST array of n_proj fp32 [T][r] as the forward call wrote them
+ *   base    : fp32 [T][K], a gradient of X that is there already (what comes through the shared projections or the routers);
+ *             NULL is zero; may be dX itself
+ *   dX      : fp32 [T][K] (out), or NULL
+ *   dA_host, dB_host : HOST arrays of n_proj fp32 [n_adapters][r][K] / [n_adapters][r][N_i] (out, written whole: zero for
+ *             adapters without a token and beyond a rank); either array may be NULL
+ *   ws      : at least mbq_lora_backward_workspace_bytes(...) bytes, 256-byte aligned, contents do not matter
+ * dX of a token without an adapter is base; its rows of X, dY and H are not used.  The gradient through the shared projection
+ * itself is the caller's (mbq_dequant gives its weights).  T = 0 is legal (dA and dB are zero-filled).
+ */
+size_t mbq_lora_backward_workspace_bytes(int64_t T, int64_t K, int n_proj, const int64_t* N_host, int64_t n_adapters,
+                                         int r);
+mbq_status mbq_lora_backward_group(const uint16_t* X, int64_t T, int64_t K, int n_proj, const uint16_t* const* A_host,
+                                   const uint16_t* const* B_host, const int64_t* N_host, int64_t n_adapters, int r,
+                                   const int32_t* ranks, const float* scale, const int32_t* adapter, const int32_t* perm,
+                                   const int32_t* offsets, const float* const* dY_host, const float* const* H_host,
+                                   const float* base, float* dX, float* const* dA_host, float* const* dB_host, void* ws,
+                                   size_t ws_bytes, void* stream);
+/*
+ * mbq_balance_loss_group - tokens per precision, and a loss that draws the choices of n_proj routers towards a target mix.
+ * For one router with logits S [T][P] (as mbq_route writes them), over the n tokens that mask keeps, with p = softmax(S) and
+ * the choice of mbq_route (the first maximum):
+ *   counts[e] = #{t : the choice of t is e},   loss = coef sum_e (counts[e] / n) mean_t(p[t][e]) / target[e]
+ *   dlogits[t][e] = d loss / d S[t][e] with the counts as constants
+ *                 = coef / n p[t][e] (u_e - sum_j u_j p[t][j]),   u_e = counts[e] / (n target[e])
+ * target = 1/P everywhere (NULL) is the usual balance loss P sum_e f_e P_e; with a target mix the sum is least where the
+ * mix is met.  Everything is computed in fp64 and rounded once.
+ *   logits_host  : HOST array of n_proj fp64 [T][P], 1 <= P <= MBQ_MAX_SLICES, 16-byte aligned for even P
+ *   mask         : uint8 [T], 0 leaves the token out, or NULL;   its logits are not used, whatever they are
+ *   target_host  : HOST array of P doubles, finite and > 0, or NULL
+ *   counts_host, loss_host, dlogits_host : HOST arrays of n_proj int32 [P], fp32 [1], fp32 [T][P]; dlogits_host may be NULL
+ *   ws           : at least mbq_balance_loss_workspace_bytes(T, n_proj) bytes, 256-byte aligned, contents do not matter
+ * No token left: counts, loss and dlogits are zero.  A logit of -inf is a precision that is off (probability 0); a NaN, a
+ * +inf or a row of -inf alone among the tokens kept makes the loss and that row's gradient NaN.  Equal calls give equal bits.
+ */
+size_t mbq_balance_loss_workspace_bytes(int64_t T, int n_proj);
+mbq_status mbq_balance_loss_group(int n_proj, const double* const* logits_host, int64_t T, int P, const uint8_t* mask,
+                                  const double* target_host, double coef, int32_t* const* counts_host,
+                                  float* const* loss_host, float* const* dlogits_host, void* ws, size_t ws_bytes,
+                                  void* stream);
+/*
+ * mbq_route_backward_group - from the logits' gradients of n_proj routers over the same X to their parameters and X:
+ *   dWr_p[e][k] = sum_t dlogits_p[t][e] X[t][k],   dbr_p[e] = sum_t dlogits_p[t][e]
+ *   dX[t][k]    = base[t][k] + sum_p sum_e dlogits_p[t][e] Wr_p[e][k]
+ *   X : bf16 [T][K], Wr_host : HOST array of n_proj fp32 [P][K] (both 16-byte aligned; K a multiple of 128)
+ *   dlogits_host : HOST array of n_proj fp32 [T][P], 1 <= P <= MBQ_MAX_SLICES
+ *   mask : uint8 [T], 0 leaves the token out (its rows of X and dlogits are not used, its dX is base), or NULL
+ *   base : fp32 [T][K] or NULL (zero), may be dX itself;   dX : fp32 [T][K] (out), or NULL
+ *   dWr_host, dbr_host : HOST arrays of n_proj fp32 [P][K] / [P] (out); either array may be NULL
+ *   ws   : at least mbq_route_backward_workspace_bytes(T, K, n_proj, P) bytes, 256-byte aligned, contents do not matter
+ * fp32 accumulate.  T = 0 is legal (dWr and dbr are zero-filled).  Equal calls give equal bits.
+ */
+size_t mbq_route_backward_workspace_bytes(int64_t T, int64_t K, int n_proj, int P);
+mbq_status mbq_route_backward_group(const uint16_t* X, int64_t T, int64_t K, int n_proj, const float* const* Wr_host, int P,
+                                    const float* const* dlogits_host, const uint8_t* mask, const float* base, float* dX,
+                                    float* const* dWr_host, float* const* dbr_host, void* ws, size_t ws_bytes,
+                                    void* stream);
+
 #ifdef __cplusplus
 }
 #endif

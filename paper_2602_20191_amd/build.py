@@ -28,6 +28,9 @@ SOURCES = [
     ("mbq_linear_decode_f4.hip", []),
     ("mbq_linear_decode_f4_ws.hip", []),
     ("mbq_linear_prefill.hip", []),
+    ("mbq_api_beside.hip", []),
+    ("mbq_lora.hip", []),
+    ("mbq_balance.hip", []),
     ("mbq_bench.hip", []),
 ]
 
