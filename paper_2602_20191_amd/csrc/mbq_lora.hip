@@ -44,7 +44,7 @@ __device__ __forceinline__ Pieces cut(const float v[8]) {
 
 // Tiles.  Tokens grouped by adapter are cut, adapter by adapter, into tiles of at most m; the tokens without one are class n.
 // Class a gets the tiles from number offsets[a] / m + a on, which is enough for its tokens whatever the groups' sizes and
-// leaves at most one tile per class empty, so tile -> class is a search among offsets (64 ways a step) and the number of
+// leaves at most one tile per class empty, so tile -> class is a search among offsets (63 ways a step) and the number of
 // tiles, T / m + n + 1, is known to the host.
 struct Tile {
   int a;      // class
@@ -56,25 +56,23 @@ __device__ __forceinline__ int clamped(int v, int most) { return v < 0 ? 0 : (v 
 __device__ __forceinline__ Tile find_tile(const int32_t* __restrict__ offsets, int n, int T, int tile, int m) {
   const int lane = threadIdx.x & 63;
   int lo = 0, span = n + 1;
-  while (span > 1) {
-    const int step = (span + 63) >> 6, a = lo + lane * step;
-    const bool reached = lane * step < span && clamped(offsets[a], T) / m + a <= tile;
-    const int k = __popcll(__ballot(reached));
-    if (k > 1) lo += (k - 1) * step;
-    span = min(step, span - (k > 1 ? (k - 1) * step : 0));
+  while (true) {
+    // 63 ways: the lane behind the last class that is asked about has where that class ends
+    const int step = (span + 62) / 63, a = lo + lane * step;
+    const int off = a <= n ? clamped(offsets[a], T) : T;
+    const int reached = max(1, (int)__popcll(__ballot(lane * step < span && off / m + a <= tile)));
+    if (step == 1) {
+      Tile t;
+      t.a = lo + reached - 1;
+      const int from = __builtin_amdgcn_readlane(off, reached - 1), end = __builtin_amdgcn_readlane(off, reached);
+      t.first = tile - (from / m + t.a);
+      t.begin = (int)min(from + (long long)t.first * m, (long long)T);
+      t.count = clamped(end - t.begin, m);
+      return t;
+    }
+    lo += (reached - 1) * step;
+    span = min(step, span - (reached - 1) * step);
   }
-  Tile t;
-  t.a = lo;
-  const int off = clamped(offsets[lo], T), end = lo < n ? clamped(offsets[lo + 1], T) : T;
-  t.first = tile - (off / m + lo);
-  const long long begin = off + (long long)t.first * m;
-  t.begin = (int)min(begin, (long long)T);
-  t.count = clamped((int)(end - t.begin), m);
-  t.a = __builtin_amdgcn_readfirstlane(t.a);
-  t.begin = __builtin_amdgcn_readfirstlane(t.begin);
-  t.count = __builtin_amdgcn_readfirstlane(t.count);
-  t.first = __builtin_amdgcn_readfirstlane(t.first);
-  return t;
 }
 __device__ __forceinline__ int token_at(const int32_t* __restrict__ perm, int T, int i) { return clamped(perm[i], T - 1); }
 // Neighbouring work items on one XCD (blocks go round the eight of them), so that a pool is read into one L2.
@@ -271,7 +269,7 @@ constexpr int kWaves = 4;
 // What the kernels have in common: the assignment, and h as it lies between them: partial[part][unit][place][16], unit = 16
 // ranks of a projection (projection-major), place = where perm has the token.
 struct TileArgs {
-  int T, n, r, rt, units, parts, tiles;  // rt: units of a projection
+  int T, n, r, rt, units, parts_log2, tiles;  // rt: units of a projection
   const int32_t *perm, *offsets, *ranks;
   const float* scale;
   float* partial;
@@ -282,20 +280,32 @@ struct ShrinkArgs {
   const void* x[MBQ_MAX_GROUP];  // one for all (forward) or one per projection
   const uint16_t* w[MBQ_MAX_GROUP];
   int64_t L[MBQ_MAX_GROUP];  // columns
-  int chunks;                // grid.y = sources * chunks; a chunk is kUnits units
-  bool shared;               // one x
+  int share[MBQ_MAX_GROUP], extra[MBQ_MAX_GROUP];  // stages of a wavefront, one more for the first `extra` of them
+  int rt_inverse;                                  // 2^16 / rt, rounded up: units are few
+  bool shared;                                     // one x
 };
 
-// Part of h = x w^T for a tile: the tokens' rows are the one operand, as they lie in memory (lane: token, eight columns), 16
-// ranks of the adapter the other.  Four wavefronts and `parts` workgroups share the columns; x is read once for up to kUnits
-// units (the projections that share it).  Bound by reading x.
+// Part of h = x w^T for a tile: the tokens' rows are the one operand, 16 ranks of the adapter the other.  A wavefront stages 64
+// columns of its rows through LDS of its own (no barrier), since the operands' lane order (a row a lane) would make every
+// 16 bytes of a load a request of its own: reading x and w straight into the operands took 40 us for q, k, v of a 70B-shaped
+// block at 4096 tokens.  The 16-byte pieces of a row lie in LDS at their number xor the row's, which spreads both accesses over the
+// banks.  Four wavefronts and `parts` workgroups share the columns; x is read once for up to kUnits units (the projections
+// that share it).  Bound by reading x.
+// kWide: rows are 16-byte aligned; else single columns are loaded, a row of 64 by a wavefront.
 template <typename In, int kUnits, bool kWide>
 __global__ __launch_bounds__(256) void lora_shrink_kernel(const ShrinkArgs s) {
-  __shared__ float red[kWaves][kUnits * 8][64];
-  const int item = xcd_item(s.t.tiles * s.t.parts);
-  if (item >= s.t.tiles * s.t.parts) return;
-  const int tile = item / s.t.parts, part = item - tile * s.t.parts;
-  const int source = blockIdx.y / s.chunks, chunk = blockIdx.y - source * s.chunks;
+  constexpr bool kExact = sizeof(In) == 2;
+  constexpr int kPer = 16 / (int)sizeof(In);     // columns of a 16-byte piece of x
+  constexpr int kCols = 64, kXPieces = kCols / kPer, kWPieces = kCols / 8;
+  constexpr int kXRows = 64 / kXPieces, kWRows = 64 / kWPieces;  // rows of a load of the wavefront
+  constexpr int kXLoads = kTile / kXRows, kWLoads = kUnits * 16 / kWRows;
+  constexpr int kXBytes = kTile * kXPieces * 16, kWBytes = kUnits * 16 * kWPieces * 16;
+  __shared__ __align__(16) char lds[kWaves * (kXBytes + kWBytes)];
+  static_assert(sizeof(lds) >= kWaves * kUnits * 8 * 64 * 4, "the sums are joined in the same LDS");
+  const int item = xcd_item(s.t.tiles << s.t.parts_log2);
+  const int tile = item >> s.t.parts_log2, part = item & ((1 << s.t.parts_log2) - 1);
+  if (tile >= s.t.tiles) return;
+  const int source = blockIdx.y, chunk = blockIdx.z;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = lane >> 4;
   const Tile at = find_tile(s.t.offsets, s.t.n, s.t.T, tile, kTile);
   if (at.a >= s.t.n || at.count == 0) return;
@@ -304,158 +314,185 @@ __global__ __launch_bounds__(256) void lora_shrink_kernel(const ShrinkArgs s) {
   const int most = s.shared ? s.t.units : s.t.rt;  // units of this source
   const int unit0 = chunk * kUnits;
   const int64_t L = s.L[source];
-  const In* x[2];
+  char* const xs = lds + wave * (kXBytes + kWBytes);
+  char* const ws = xs + kXBytes;
+  const auto x_row = [&](int row) {
+    return static_cast<const In*>(s.x[source]) + (int64_t)token_at(s.t.perm, s.t.T, at.begin + min(row, at.count - 1)) * L;
+  };
+  const auto w_row = [&](int row) {  // rows that are not there repeat others, whose sums are not used
+    const int unit = min(unit0 + (row >> 4), most - 1), p = s.shared ? unit * s.rt_inverse >> 16 : source;
+    return s.w[p] + ((int64_t)at.a * s.t.r + min(16 * (s.shared ? unit - p * s.t.rt : unit) + (row & 15), own - 1)) * L;
+  };
+  const auto x_at = [&](int row, int piece) { return xs + (row * kXPieces + (piece ^ (row & (kXPieces - 1)))) * 16; };
+  const auto w_at = [&](int row, int piece) { return ws + (row * kWPieces + (piece ^ (row & (kWPieces - 1)))) * 16; };
+
+  const In* x[kWide ? kXLoads : 1];
+  const uint16_t* w[kWide ? kWLoads : 1];
+  if constexpr (kWide) {
 #pragma unroll
-  for (int h = 0; h < 2; ++h)
-    x[h] = static_cast<const In*>(s.x[source]) +
-           (int64_t)token_at(s.t.perm, s.t.T, at.begin + min(16 * h + (lane & 15), at.count - 1)) * L + 8 * q;
-  const uint16_t* w[kUnits];
+    for (int i = 0; i < kXLoads; ++i) x[i] = x_row(i * kXRows + lane / kXPieces) + lane % kXPieces * kPer;
 #pragma unroll
-  for (int u = 0; u < kUnits; ++u) {
-    const int unit = min(unit0 + u, most - 1), p = s.shared ? unit / s.t.rt : source;
-    const int j = min(16 * (s.shared ? unit - p * s.t.rt : unit) + (lane & 15), own - 1);
-    w[u] = s.w[p] + ((int64_t)at.a * s.t.r + j) * L + 8 * q;
+    for (int i = 0; i < kWLoads; ++i) w[i] = w_row(i * kWRows + lane / kWPieces) + lane % kWPieces * 8;
   }
+  uint4 xv[kXLoads], wv[kWLoads];
+  const auto load = [&](int64_t k) {
+    if (k + kCols <= L) {
+#pragma unroll
+      for (int i = 0; i < kXLoads; ++i) xv[i] = *reinterpret_cast<const uint4*>(x[i] + k);
+#pragma unroll
+      for (int i = 0; i < kWLoads; ++i) wv[i] = *reinterpret_cast<const uint4*>(w[i] + k);
+    } else {  // the last columns: pieces are there or not as a whole
+#pragma unroll
+      for (int i = 0; i < kXLoads; ++i) {
+        xv[i] = uint4{0, 0, 0, 0};
+        if (k + lane % kXPieces * kPer < L) xv[i] = *reinterpret_cast<const uint4*>(x[i] + k);
+      }
+#pragma unroll
+      for (int i = 0; i < kWLoads; ++i) {
+        wv[i] = uint4{0, 0, 0, 0};
+        if (k + lane % kWPieces * 8 < L) wv[i] = *reinterpret_cast<const uint4*>(w[i] + k);
+      }
+    }
+  };
+  const auto store = [&](int64_t k) {
+    if constexpr (kWide) {
+#pragma unroll
+      for (int i = 0; i < kXLoads; ++i) *reinterpret_cast<uint4*>(x_at(i * kXRows + lane / kXPieces, lane % kXPieces)) = xv[i];
+#pragma unroll
+      for (int i = 0; i < kWLoads; ++i) *reinterpret_cast<uint4*>(w_at(i * kWRows + lane / kWPieces, lane % kWPieces)) = wv[i];
+    } else {
+      const bool there = k + lane < L;
+#pragma unroll 8
+      for (int row = 0; row < kTile; ++row)
+        reinterpret_cast<In*>(x_at(row, lane / kPer))[lane % kPer] = there ? x_row(row)[k + lane] : In(0);
+#pragma unroll 8
+      for (int row = 0; row < 16 * kUnits; ++row)
+        reinterpret_cast<uint16_t*>(w_at(row, lane / 8))[lane % 8] = there ? w_row(row)[k + lane] : uint16_t(0);
+    }
+  };
   floatx4 acc[kUnits][2];
 #pragma unroll
   for (int u = 0; u < kUnits; ++u) acc[u][0] = acc[u][1] = floatx4{0.f, 0.f, 0.f, 0.f};
-
-  // a step is 32 columns from column k on; left: columns of the lane's eight that exist (8 but in the last step)
-  constexpr bool kExact = sizeof(In) == 2;
-  constexpr int kAhead = kExact ? 4 : 2;  // steps whose loads are on their way together
-  struct Step {
-    uint4 w[kUnits];
-    uint4 x[2][kExact ? 1 : 2];
-  };
-  const auto load = [&](Step& st, int64_t k, int left) {
+  const auto use = [&]() {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      if constexpr (kExact) {
-        st.x[h][0] = *reinterpret_cast<const uint4*>(x[h] + k);
-      } else if constexpr (kWide) {
-        st.x[h][0] = st.x[h][1] = uint4{0, 0, 0, 0};
-        if (left > 0) {
-          st.x[h][0] = *reinterpret_cast<const uint4*>(x[h] + k);
-          st.x[h][1] = *reinterpret_cast<const uint4*>(x[h] + k + 4);
-        }
-      } else {
-        uint32_t v[8];
+    for (int k = 0; k < kCols / 32; ++k) {
+      uint4 wf[kUnits];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = e < left ? __float_as_uint(x[h][k + e]) : 0u;
-        st.x[h][0] = uint4{v[0], v[1], v[2], v[3]};
-        st.x[h][1] = uint4{v[4], v[5], v[6], v[7]};
-      }
-    }
+      for (int u = 0; u < kUnits; ++u) wf[u] = *reinterpret_cast<const uint4*>(w_at(16 * u + (lane & 15), 4 * k + q));
 #pragma unroll
-    for (int u = 0; u < kUnits; ++u) {
-      if constexpr (kWide) {
-        st.w[u] = *reinterpret_cast<const uint4*>(w[u] + (left > 0 ? k : -8 * q));
-      } else {
-        uint32_t v[8];
+      for (int h = 0; h < 2; ++h) {
+        const int row = 16 * h + (lane & 15);
+        if constexpr (kExact) {
+          const uint4 xf = *reinterpret_cast<const uint4*>(x_at(row, 4 * k + q));
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = w[u][e < left ? k + e : -8 * q];
-        st.w[u] = uint4{v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16};
-      }
-    }
-  };
-  const auto use = [&](const Step& st) {
+          for (int u = 0; u < kUnits; ++u) acc[u][h] = bf::mfma(xf, wf[u], acc[u][h]);
+        } else {
+          const float4 a = *reinterpret_cast<const float4*>(x_at(row, 8 * k + 2 * q));
+          const float4 b = *reinterpret_cast<const float4*>(x_at(row, 8 * k + 2 * q + 1));
+          const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+          const Pieces pc = cut(v);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      if constexpr (kExact) {
-#pragma unroll
-        for (int u = 0; u < kUnits; ++u) acc[u][h] = bf::mfma(st.x[h][0], st.w[u], acc[u][h]);
-      } else {
-        const uint4 a = st.x[h][0], b = st.x[h][1];
-        const float v[8] = {__uint_as_float(a.x), __uint_as_float(a.y), __uint_as_float(a.z), __uint_as_float(a.w),
-                            __uint_as_float(b.x), __uint_as_float(b.y), __uint_as_float(b.z), __uint_as_float(b.w)};
-        const Pieces pc = cut(v);
-#pragma unroll
-        for (int u = 0; u < kUnits; ++u) {
-          acc[u][h] = bf::mfma(pc.lo, st.w[u], acc[u][h]);
-          acc[u][h] = bf::mfma(pc.mid, st.w[u], acc[u][h]);
-          acc[u][h] = bf::mfma(pc.hi, st.w[u], acc[u][h]);
+          for (int u = 0; u < kUnits; ++u) {
+            acc[u][h] = bf::mfma(pc.lo, wf[u], acc[u][h]);
+            acc[u][h] = bf::mfma(pc.mid, wf[u], acc[u][h]);
+            acc[u][h] = bf::mfma(pc.hi, wf[u], acc[u][h]);
+          }
         }
       }
     }
   };
-  const int64_t steps = L >> 5, shares = (int64_t)s.t.parts * kWaves, share = (int64_t)part * kWaves + wave;
-  int64_t k = (steps * share / shares) << 5;
-  const int64_t k1 = (steps * (share + 1) / shares) << 5;
-  for (; k + 32 * kAhead <= k1; k += 32 * kAhead) {
-    Step st[kAhead];
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) load(st[i], k + 32 * i, 8);
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) use(st[i]);
+  const int share = part * kWaves + wave, first = share * s.share[source] + min(share, s.extra[source]);
+  const int64_t k0 = (int64_t)first * kCols, k1 = k0 + (s.share[source] + (share < s.extra[source] ? 1 : 0)) * kCols;
+  if (kWide && k0 < k1) load(k0);
+  for (int64_t k = k0; k < k1; k += kCols) {
+    store(k);
+    if (kWide && k + kCols < k1) load(k + kCols);
+    use();
   }
-  for (; k < k1; k += 32) {
-    Step st;
-    load(st, k, 8);
-    use(st);
-  }
-  if constexpr (!kExact) {  // (K is a multiple of 128)
-    if (share == shares - 1 && (L & 31)) {
-      Step st;
-      load(st, steps << 5, clamped((int)(L & 31) - 8 * q, 8));
-      use(st);
-    }
-  }
+  __syncthreads();
+  float* const red = reinterpret_cast<float*>(lds);  // [wave][value][lane]
 #pragma unroll
   for (int u = 0; u < kUnits; ++u)
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) red[wave][(u * 2 + h) * 4 + i][lane] = acc[u][h][i];
+      for (int i = 0; i < 4; ++i) red[((wave * kUnits + u) * 8 + h * 4 + i) * 64 + lane] = acc[u][h][i];
   __syncthreads();
 #pragma unroll
-  for (int e = threadIdx.x; e < kUnits * 512; e += 256) {
-    const int value = e >> 6, l = e & 63, u = value >> 3, h = (value >> 2) & 1, i = value & 3;
-    if (unit0 + u >= most) continue;
-    const float sum = (red[0][value][l] + red[1][value][l]) + (red[2][value][l] + red[3][value][l]);
-    const int unit = s.shared ? unit0 + u : source * s.t.rt + unit0 + u;
-    const int token = 16 * h + 4 * (l >> 4) + i;
-    if (token < at.count)
-      s.t.partial[(((int64_t)part * s.t.units + unit) * s.t.T + at.begin + token) * 16 + (l & 15)] = sum;
-  }
-}
-
-// Eight ranks from j on of the token at a place, summed over the parts.
-__device__ __forceinline__ void whole_h(const TileArgs& t, int p, int place, int j, float v[8]) {
-  const float* at = t.partial + ((int64_t)(p * t.rt + (j >> 4)) * t.T + place) * 16 + (j & 15);
+  for (int e = threadIdx.x; e < kUnits * 128; e += 256) {  // four ranks of a token
+    const int u = e >> 7, token = (e >> 2) & 31, j = 4 * (e & 3);
+    const int from = ((u * 8 + (token >> 4) * 4 + (token & 3)) * 64) + ((token >> 2) & 3) * 16 + j;
+    if (unit0 + u >= most || token >= at.count) continue;
+    float4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = 0.f;
-  for (int s = 0; s < t.parts; ++s) {
-    const float4 a = *reinterpret_cast<const float4*>(at), b = *reinterpret_cast<const float4*>(at + 4);
-    v[0] += a.x, v[1] += a.y, v[2] += a.z, v[3] += a.w, v[4] += b.x, v[5] += b.y, v[6] += b.z, v[7] += b.w;
-    at += (int64_t)t.units * t.T * 16;
+    for (int i = 0; i < kWaves; ++i) {
+      const float4 v = *reinterpret_cast<const float4*>(red + i * (kUnits * 512) + from);
+      sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w;
+    }
+    const int unit = (s.shared ? 0 : source * s.t.rt) + unit0 + u;
+    *reinterpret_cast<float4*>(s.t.partial + (((int64_t)part * s.t.units + unit) * s.t.T + at.begin + token) * 16 + j) = sum;
   }
 }
 
+// Four ranks from j on of the token at a place, summed over the parts (in order, four loads on their way at a time).
+__device__ __forceinline__ float4 whole_h(const TileArgs& t, int p, int place, int j) {
+  const float* at = t.partial + ((int64_t)(p * t.rt + (j >> 4)) * t.T + place) * 16 + (j & 15);
+  const int64_t next = (int64_t)t.units * t.T * 16;
+  const int parts = 1 << t.parts_log2;
+  float4 sum = {0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < parts; s += 4) {
+    float4 v[4] = {};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (s + i < parts) v[i] = *reinterpret_cast<const float4*>(at + (s + i) * next);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum.x += v[i].x, sum.y += v[i].y, sum.z += v[i].z, sum.w += v[i].w;
+  }
+  return sum;
+}
+
+// What is read and written once and is more than the L2 caches hold goes past them: the reads of the launches that follow
+// do not then wait for dirty lines to leave (q, k, v of a 70B-shaped block at 4096 tokens 119 -> 106 us).
+template <bool kStream>
+__device__ __forceinline__ floatx4 load4(const float* p) {
+  if constexpr (kStream) return __builtin_nontemporal_load(reinterpret_cast<const floatx4*>(p));
+  return *reinterpret_cast<const floatx4*>(p);
+}
+template <bool kStream>
+__device__ __forceinline__ void store4(float* p, floatx4 v) {
+  if constexpr (kStream)
+    __builtin_nontemporal_store(v, reinterpret_cast<floatx4*>(p));
+  else
+    *reinterpret_cast<floatx4*>(p) = v;
+}
+
+constexpr int kExpandColumns = 256;  // of a workgroup
 struct ExpandArgs {
   TileArgs t;
   const uint16_t* w[MBQ_MAX_GROUP];
   const float* base[MBQ_MAX_GROUP];
   float *y[MBQ_MAX_GROUP], *H[MBQ_MAX_GROUP];
   int64_t L[MBQ_MAX_GROUP];
-  int blocks;   // of columns, of the widest output
-  int sources;  // projections that add to one output: 1 (forward: output blockIdx.y), or all (backward: output 0)
+  int outputs, first[MBQ_MAX_GROUP], blocks;  // blocks of columns: an output's first, of all of them
+  int sources;  // projections that add to one output: 1 (forward: the output's own), or all (backward, one output)
 };
 
-// y = base + sum over the sources of scale h w for a tile.  h, cut into pieces, goes through LDS (lane: token, eight ranks); w
-// is turned in registers: a lane loads four neighbouring columns of eight ranks and pairs ranks up by one byte permutation a
-// dword, so MFMA c of a set of four yields columns 4 (lane mod 16) + c, and a lane's four results of one token are one 16-byte
-// access to base and y.  Bound by reading base and writing y.
-template <int kSub, bool kWide>
+// y = base + sum over the sources of scale h w for a tile.  h, cut into pieces, goes through LDS 32 ranks at a time (lane:
+// token, eight ranks); w is turned in registers: a lane loads four columns of eight ranks and pairs ranks up by one byte
+// permutation a dword.  kWide: MFMA c of a set of four yields columns 4 (lane mod 16) + c, so that a lane's four results of
+// one token are one 16-byte access to base and y; else columns 16 c + lane mod 16.  base, and the next step's h and w, are on
+// their way while a step is multiplied.  Bound by reading base and writing y.
+template <bool kWide, bool kStream>
 __global__ __launch_bounds__(256) void lora_expand_kernel(const ExpandArgs s) {
-  constexpr int kStage = 64, kStride = kStage + 8;  // ranks in LDS at a time
-  __shared__ __align__(16) uint16_t pieces[3][kTile][kStride];
-  __shared__ int rows[kTile];
+  constexpr int kStep = 32, kStride = kStep + 8;
+  __shared__ __align__(16) uint16_t pieces[2][3][kTile][kStride];
   const int item = xcd_item(s.t.tiles * s.blocks);
   if (item >= s.t.tiles * s.blocks) return;
-  const int tile = item / s.blocks, block = item - tile * s.blocks;
-  const int out = s.sources == 1 ? blockIdx.y : 0;
+  const int tile = item / s.blocks;
+  int block = item - tile * s.blocks, out = 0;
+  while (out + 1 < s.outputs && block >= s.first[out + 1]) ++out;
+  block -= s.first[out];
   const int64_t L = s.L[out];
-  if ((int64_t)block * (256 * kSub) >= L) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, q = lane >> 4;
   const Tile at = find_tile(s.t.offsets, s.t.n, s.t.T, tile, kTile);
   if (at.count == 0) return;
@@ -465,134 +502,157 @@ __global__ __launch_bounds__(256) void lora_expand_kernel(const ExpandArgs s) {
   const float* base = s.base[out];
   float* y = s.y[out];
   float* H = block == 0 ? s.H[out] : nullptr;
-  if (tid < kTile) rows[tid] = token_at(s.t.perm, s.t.T, at.begin + min(tid, at.count - 1));
-  const int64_t c0 = (int64_t)block * (256 * kSub) + wave * (64 * kSub) + 4 * (lane & 15);
+  const int64_t c0 = (int64_t)block * kExpandColumns + wave * 64 + (lane & 15) * (kWide ? 4 : 1);
+  const auto column = [&](int c) { return c0 + (kWide ? c : 16 * c); };
+  const int place = at.begin + min(tid >> 3, at.count - 1);  // of the thread's token of h
 
-  floatx4 acc[kSub][2][4];
+  int64_t to[2][4];  // a lane's four tokens of either half
 #pragma unroll
-  for (int b = 0; b < kSub; ++b)
+  for (int h = 0; h < 2; ++h)
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int c = 0; c < 4; ++c) acc[b][h][c] = floatx4{0.f, 0.f, 0.f, 0.f};
-
-  __syncthreads();
-  if (H && own == 0)
-    for (int e = tid; e < at.count * s.t.r; e += 256) H[(int64_t)rows[e / s.t.r] * s.t.r + e % s.t.r] = 0.f;
-  const int p0 = s.sources == 1 ? out : 0;
-  for (int p = p0; p < p0 + s.sources; ++p) {
-    const uint16_t* w = s.w[p] + (some ? (int64_t)at.a * s.t.r * L : 0);
-    for (int j0 = 0; j0 < (H && own ? s.t.r : own); j0 += kStage) {
-      {  // thread: token tid / 8, eight ranks
-        const int token = tid >> 3, j = j0 + 8 * (tid & 7);
-        float v[8] = {};
-        if (j < own && token < at.count) whole_h(s.t, p, at.begin + token, j, v);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          if (j + e >= own) v[e] = 0.f;
-          if (H && j + e < s.t.r && token < at.count) H[(int64_t)rows[token] * s.t.r + j + e] = v[e];
-          v[e] *= scale;
-        }
-        const Pieces pc = cut(v);
-        *reinterpret_cast<uint4*>(&pieces[0][token][8 * (tid & 7)]) = pc.lo;
-        *reinterpret_cast<uint4*>(&pieces[1][token][8 * (tid & 7)]) = pc.mid;
-        *reinterpret_cast<uint4*>(&pieces[2][token][8 * (tid & 7)]) = pc.hi;
-      }
-      __syncthreads();
-      for (int k = 0; k < kStage && j0 + k < own; k += 32) {
-        uint4 hv[3][2];
-#pragma unroll
-        for (int i = 0; i < 3; ++i)
-#pragma unroll
-          for (int h = 0; h < 2; ++h) hv[i][h] = *reinterpret_cast<const uint4*>(&pieces[i][16 * h + (lane & 15)][k + 8 * q]);
-#pragma unroll
-        for (int b = 0; b < kSub; ++b) {
-          const int64_t c = c0 + 64 * b;
-          uint2 v[8];  // four columns of ranks j0 + k + 8 q ..; ranks that are not there meet zeros
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const uint16_t* row = w + (int64_t)min(j0 + k + 8 * q + e, own - 1) * L;
-            if constexpr (kWide) {
-              v[e] = *reinterpret_cast<const uint2*>(row + min(c, L - 4));
-            } else {
-              v[e].x = row[min(c, L - 1)] | (uint32_t)row[min(c + 1, L - 1)] << 16;
-              v[e].y = row[min(c + 2, L - 1)] | (uint32_t)row[min(c + 3, L - 1)] << 16;
-            }
-          }
-#pragma unroll
-          for (int col = 0; col < 4; ++col) {
-            uint32_t d[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const uint32_t even = col < 2 ? v[2 * e].x : v[2 * e].y, odd = col < 2 ? v[2 * e + 1].x : v[2 * e + 1].y;
-              d[e] = __builtin_amdgcn_perm(odd, even, col & 1 ? 0x07060302u : 0x05040100u);
-            }
-            const uint4 wv = {d[0], d[1], d[2], d[3]};
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-              for (int i = 0; i < 3; ++i) acc[b][h][col] = bf::mfma(hv[i][h], wv, acc[b][h][col]);
-          }
-        }
-      }
-      __syncthreads();
-    }
-  }
-  if (own == 0 && y == base) return;
-#pragma unroll
-  for (int b = 0; b < kSub; ++b) {
-    const int64_t c = c0 + 64 * b;
-    if (c >= L) continue;
+    for (int i = 0; i < 4; ++i)
+      to[h][i] = (int64_t)token_at(s.t.perm, s.t.T, at.begin + min(16 * h + 4 * q + i, at.count - 1)) * L;
+  const auto there = [&](int h, int i) { return 16 * h + 4 * q + i < at.count; };
+  floatx4 b[2][4];
+  const bool copies = !(own == 0 && y == base);
+  if (copies) {
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int token = 16 * h + 4 * q + i;
-        if (token >= at.count) continue;
-        const int64_t to = (int64_t)rows[token] * L + c;
+        b[h][i] = floatx4{0.f, 0.f, 0.f, 0.f};
+        if (!base || !there(h, i)) continue;
         if constexpr (kWide) {
-          float4 v = base ? *reinterpret_cast<const float4*>(base + to) : float4{0.f, 0.f, 0.f, 0.f};
-          v.x += acc[b][h][0][i], v.y += acc[b][h][1][i], v.z += acc[b][h][2][i], v.w += acc[b][h][3][i];
-          *reinterpret_cast<float4*>(y + to) = v;
+          if (c0 < L) b[h][i] = load4<kStream>(base + to[h][i] + c0);
         } else {
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (c + e < L) y[to + e] = (base ? base[to + e] : 0.f) + acc[b][h][e][i];
+          for (int c = 0; c < 4; ++c)
+            if (column(c) < L) b[h][i][c] = base[to[h][i] + column(c)];
         }
       }
   }
+  floatx4 acc[2][4];
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) acc[h][c] = floatx4{0.f, 0.f, 0.f, 0.f};
+
+  // steps of 32 ranks, source by source
+  const int p0 = s.sources == 1 ? out : 0, per = (own + kStep - 1) / kStep, steps = per * s.sources;
+  float4 hv;
+  uint2 wv[8];  // four columns of ranks 8 q ..
+  const auto load = [&](int p, int j0) {
+    const int j = j0 + 4 * (tid & 7);
+    hv = float4{0.f, 0.f, 0.f, 0.f};
+    if (j < own) hv = whole_h(s.t, p, place, j);
+    const uint16_t* w = s.w[p] + (int64_t)at.a * s.t.r * L;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {  // ranks that are not there meet zeros
+      const uint16_t* row = w + (int64_t)min(j0 + 8 * q + e, own - 1) * L;
+      if constexpr (kWide) {
+        wv[e] = *reinterpret_cast<const uint2*>(row + min(c0, L - 4));
+      } else {
+        wv[e].x = row[min(column(0), L - 1)] | (uint32_t)row[min(column(1), L - 1)] << 16;
+        wv[e].y = row[min(column(2), L - 1)] | (uint32_t)row[min(column(3), L - 1)] << 16;
+      }
+    }
+  };
+  if (steps) load(p0, 0);
+  int p = p0, j0 = 0;
+  for (int step = 0; step < steps; ++step) {
+    {
+      const int j = j0 + 4 * (tid & 7);
+      float v[4] = {hv.x, hv.y, hv.z, hv.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (j + e >= own) v[e] = 0.f;
+        if (H && j + e < s.t.r && (tid >> 3) < at.count)
+          H[(int64_t)token_at(s.t.perm, s.t.T, place) * s.t.r + j + e] = v[e];
+        v[e] *= scale;
+      }
+      uint2 pc[3];
+      cut_pair(v[0], v[1], pc[2].x, pc[1].x, pc[0].x);
+      cut_pair(v[2], v[3], pc[2].y, pc[1].y, pc[0].y);
+#pragma unroll
+      for (int i = 0; i < 3; ++i) *reinterpret_cast<uint2*>(&pieces[step & 1][i][tid >> 3][4 * (tid & 7)]) = pc[i];
+    }
+    uint4 w4[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      uint32_t d[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t even = c < 2 ? wv[2 * e].x : wv[2 * e].y, odd = c < 2 ? wv[2 * e + 1].x : wv[2 * e + 1].y;
+        d[e] = __builtin_amdgcn_perm(odd, even, c & 1 ? 0x07060302u : 0x05040100u);
+      }
+      w4[c] = uint4{d[0], d[1], d[2], d[3]};
+    }
+    j0 += kStep;
+    if (j0 >= own) ++p, j0 = 0;
+    if (step + 1 < steps) load(p, j0);
+    __syncthreads();  // (the other buffer's readers passed the barrier before: two buffers do)
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        const uint4 a = *reinterpret_cast<const uint4*>(&pieces[step & 1][i][16 * h + (lane & 15)][8 * q]);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) acc[h][c] = bf::mfma(a, w4[c], acc[h][c]);
+      }
+  }
+  if (H)  // ranks that are not there
+    for (int e = tid; e < at.count * s.t.r; e += 256) {
+      const int j = e % s.t.r;
+      if (j >= per * kStep) H[(int64_t)token_at(s.t.perm, s.t.T, at.begin + e / s.t.r) * s.t.r + j] = 0.f;
+    }
+  if (!copies) return;
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (!there(h, i)) continue;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) b[h][i][c] += acc[h][c][i];
+      if constexpr (kWide) {
+        if (c0 < L) store4<kStream>(y + to[h][i] + c0, b[h][i]);
+      } else {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          if (column(c) < L) y[to[h][i] + column(c)] = b[h][i][c];
+      }
+    }
 }
 
 // The operands of the gradients' products over tokens: fragments[projection][tile][unit of the projection][piece][lane] holds
 // 16 bytes, rank 16 unit + lane mod 16 of tokens 8 (lane / 16) .. + 7 of the tile; tokens that are not there are zero.  One
-// wavefront per (tile, projection): of g (summed over its parts) or of h as the forward pass left it, times the scale.
+// wavefront per (tile, projection, unit): of g (summed over its parts) or of h as the forward pass left it, times the scale.
 struct FragmentArgs {
   TileArgs t;
   const float* h[MBQ_MAX_GROUP];  // null: g from t.partial
   uint4* fragments;
 };
 __global__ __launch_bounds__(64) void lora_fragment_kernel(const FragmentArgs s) {
-  const int tile = blockIdx.x, p = blockIdx.y, lane = threadIdx.x, q = lane >> 4;
+  const int tile = blockIdx.x, p = blockIdx.y, unit = blockIdx.z, lane = threadIdx.x, q = lane >> 4;
   const Tile at = find_tile(s.t.offsets, s.t.n, s.t.T, tile, kTile);
   if (at.a >= s.t.n || at.count == 0) return;
   const int own = own_rank(s.t.ranks, at.a, s.t.r);
   const float scale = s.t.scale[at.a];
-  for (int unit = 0; unit < s.t.rt; ++unit) {
+  {
     const int j = 16 * unit + (lane & 15);
     float v[8] = {};
     if (j < own) {
+      if (s.h[p]) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int token = 8 * q + e;
-        if (token >= at.count) continue;
-        if (s.h[p]) {
-          v[e] = s.h[p][(int64_t)token_at(s.t.perm, s.t.T, at.begin + token) * s.t.r + j];
-        } else {
-          const float* from = s.t.partial + ((int64_t)(p * s.t.rt + unit) * s.t.T + at.begin + token) * 16 + (lane & 15);
-          for (int i = 0; i < s.t.parts; ++i) v[e] += from[(int64_t)i * s.t.units * s.t.T * 16];
-        }
-        v[e] *= scale;
+        for (int e = 0; e < 8; ++e)
+          v[e] = s.h[p][(int64_t)token_at(s.t.perm, s.t.T, at.begin + min(8 * q + e, at.count - 1)) * s.t.r + j];
+      } else {
+        const float* from = s.t.partial + ((int64_t)(p * s.t.rt + unit) * s.t.T + at.begin) * 16 + (lane & 15);
+        for (int i = 0; i < 1 << s.t.parts_log2; ++i, from += (int64_t)s.t.units * s.t.T * 16)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] += from[min(8 * q + e, at.count - 1) * 16];
       }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = 8 * q + e < at.count ? v[e] * scale : 0.f;
     }
     const Pieces pc = cut(v);
     uint4* to = s.fragments + (((int64_t)p * s.t.tiles + tile) * s.t.rt + unit) * 192 + lane;
@@ -742,6 +802,8 @@ __global__ __launch_bounds__(256) void lora_join_kernel(const JoinArgs s) {
 // ---- launches ---------------------------------------------------------------------------------------------------
 namespace {
 
+constexpr int64_t kCacheBytes = 32 << 20;  // the eight L2 caches
+
 int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
 TileArgs tile_args(const LoraCall& c) {
@@ -758,15 +820,20 @@ TileArgs tile_args(const LoraCall& c) {
   t.scale = c.scale;
   return t;
 }
-// Parts along the columns: enough workgroups for two a compute unit at the tiles that hold tokens, and at least two steps of
-// 32 columns per wavefront.
-int shrink_parts(int64_t T, int64_t L) {
+// Parts along the columns (their log2): about two workgroups a compute unit at the tiles that hold tokens, and at least a
+// stage of 64 columns per wavefront.
+int shrink_parts_log2(int64_t T, int64_t L) {
   const int64_t tiles = up(T, kTile) / kTile;
-  int64_t parts = (512 + tiles - 1) / tiles;
-  parts = parts < L / (kWaves * 64) ? parts : L / (kWaves * 64);
-  return (int)(parts < 1 ? 1 : parts > 16 ? 16 : parts);
+  int parts = 0;
+  while (parts < 4 && (tiles << parts) < 384 && (kWaves * 64 << (parts + 1)) <= L) ++parts;
+  return parts;
 }
-size_t partial_bytes(int64_t T, int units, int parts) { return (size_t)T * units * parts * 64; }
+void shrink_shares(ShrinkArgs* s, int source) {
+  const int64_t stages = up(s->L[source], 64) / 64, shares = (int64_t)kWaves << s->t.parts_log2;
+  s->share[source] = (int)(stages / shares);
+  s->extra[source] = (int)(stages % shares);
+}
+size_t partial_bytes(int64_t T, int units, int parts_log2) { return ((size_t)T * units * 64) << parts_log2; }
 int decode_parts(int64_t K, int* columns) {
   const int64_t passes = up(K, kDecodeColumns) / kDecodeColumns, each = (passes + 15) / 16;
   *columns = (int)(each * kDecodeColumns);
@@ -775,8 +842,8 @@ int decode_parts(int64_t K, int* columns) {
 
 template <typename In, bool kWide>
 void shrink(const ShrinkArgs& s, int sources, hipStream_t stream) {
-  const dim3 grid(xcd_blocks((int64_t)s.t.tiles * s.t.parts), (unsigned)(sources * s.chunks));
   const int units = s.shared ? s.t.units : s.t.rt;
+  const dim3 grid(xcd_blocks((int64_t)s.t.tiles << s.t.parts_log2), sources, (units + 3) / 4);
   if (units == 1)
     hipLaunchKernelGGL((lora_shrink_kernel<In, 1, kWide>), grid, dim3(256), 0, stream, s);
   else if (units == 2)
@@ -786,21 +853,23 @@ void shrink(const ShrinkArgs& s, int sources, hipStream_t stream) {
   else
     hipLaunchKernelGGL((lora_shrink_kernel<In, 4, kWide>), grid, dim3(256), 0, stream, s);
 }
-int shrink_chunks(int units) { return (units + 3) / 4; }
 
 void expand(const ExpandArgs& s0, int outputs, bool w, hipStream_t stream) {
   ExpandArgs s = s0;
-  int64_t most = 0;
-  for (int i = 0; i < outputs; ++i) most = s.L[i] > most ? s.L[i] : most;
-  const bool two = w && most * s.t.T >= (int64_t)512 * 512 * kTile;  // 512 columns a workgroup where that leaves two a compute unit
-  s.blocks = (int)(up(most, two ? 512 : 256) / (two ? 512 : 256));
-  const dim3 grid(xcd_blocks((int64_t)s.t.tiles * s.blocks), (unsigned)outputs);
-  if (w && two)
-    hipLaunchKernelGGL((lora_expand_kernel<2, true>), grid, dim3(256), 0, stream, s);
-  else if (w)
-    hipLaunchKernelGGL((lora_expand_kernel<1, true>), grid, dim3(256), 0, stream, s);
+  int64_t columns = 0;
+  s.outputs = outputs;
+  for (int i = 0; i < outputs; ++i) {
+    s.first[i] = s.blocks;
+    s.blocks += (int)(up(s.L[i], kExpandColumns) / kExpandColumns);
+    columns += s.L[i];
+  }
+  const dim3 grid(xcd_blocks((int64_t)s.t.tiles * s.blocks));
+  if (!w)
+    hipLaunchKernelGGL((lora_expand_kernel<false, false>), grid, dim3(256), 0, stream, s);
+  else if (s.t.T * columns * 4 > kCacheBytes)
+    hipLaunchKernelGGL((lora_expand_kernel<true, true>), grid, dim3(256), 0, stream, s);
   else
-    hipLaunchKernelGGL((lora_expand_kernel<1, false>), grid, dim3(256), 0, stream, s);
+    hipLaunchKernelGGL((lora_expand_kernel<true, false>), grid, dim3(256), 0, stream, s);
 }
 
 template <typename In, bool kWide>
@@ -825,7 +894,7 @@ int64_t blocks_of(int64_t L, int width) { return up(L, width) / width; }
 constexpr int kWidthX = 128, kWidthY = 64;  // columns of a workgroup of lora_outer_kernel: bf16, fp32
 
 struct BackwardPlan {
-  int parts, chunk_x, chunk_y;
+  int parts_log2, chunk_x, chunk_y;
   size_t partial, fragments, more_x, more_y[MBQ_MAX_GROUP];  // bytes; fragments: of g or of h
   size_t bytes;
 };
@@ -837,10 +906,10 @@ BackwardPlan backward_plan(int64_t T, int64_t K, int n, const int64_t* N, int64_
     most = N[p] > most ? N[p] : most;
     blocks += blocks_of(N[p], kWidthY);
   }
-  b.parts = shrink_parts(T, most);
+  b.parts_log2 = shrink_parts_log2(T, most);
   b.chunk_x = outer_chunk(T, blocks_of(K, kWidthX) * n * groups, r);
   b.chunk_y = outer_chunk(T, blocks * groups, r);
-  b.partial = up((int64_t)partial_bytes(T, rt * n, b.parts), 256);
+  b.partial = up((int64_t)partial_bytes(T, rt * n, b.parts_log2), 256);
   b.fragments = (size_t)n * (T / kTile + adapters + 1) * rt * 3072;
   b.more_x = up((int64_t)((T - 1) / b.chunk_x + 1) * r * K * 4, 256);
   b.bytes = b.partial + 2 * b.fragments;
@@ -856,7 +925,7 @@ BackwardPlan backward_plan(int64_t T, int64_t K, int n, const int64_t* N, int64_
 size_t lora_workspace_bytes(int64_t T, int64_t K, int n, int r) {
   int columns;
   if (T <= kDecodeTokens) return (size_t)T * n * r * decode_parts(K, &columns) * 4 + 256;
-  return partial_bytes(T, (r + 15) / 16 * n, shrink_parts(T, K)) + 256;
+  return partial_bytes(T, (r + 15) / 16 * n, shrink_parts_log2(T, K)) + 256;
 }
 
 mbq_status launch_lora(const LoraCall& c, hipStream_t stream) {
@@ -895,11 +964,12 @@ mbq_status launch_lora(const LoraCall& c, hipStream_t stream) {
   ShrinkArgs s = {};
   s.t = tile_args(c);
   s.t.partial = reinterpret_cast<float*>(c.ws);
-  s.t.parts = shrink_parts(c.T, c.K);
+  s.t.parts_log2 = shrink_parts_log2(c.T, c.K);
   s.shared = true;
+  s.rt_inverse = (65535 + s.t.rt) / s.t.rt;
   s.x[0] = c.X;
   s.L[0] = c.K;
-  s.chunks = shrink_chunks(s.t.units);
+  shrink_shares(&s, 0);
   ExpandArgs e = {};
   bool w = true;
   for (int p = 0; p < c.n; ++p) {
@@ -938,13 +1008,13 @@ mbq_status launch_lora_backward(const LoraCall& c, hipStream_t stream) {
   ShrinkArgs s = {};
   s.t = tile_args(c);
   s.t.partial = reinterpret_cast<float*>(c.ws);
-  s.t.parts = plan.parts;
-  s.chunks = shrink_chunks(s.t.rt);
+  s.t.parts_log2 = plan.parts_log2;
   bool w = true, wy = true;
   for (int p = 0; p < c.n; ++p) {
     s.x[p] = c.dY[p];
     s.w[p] = c.B[p];
     s.L[p] = c.N[p];
+    shrink_shares(&s, p);
     wy = wy && wide(c.dY[p], c.N[p], 4, 16);
     w = w && wide(c.B[p], c.N[p], 8, 16);
   }
@@ -977,7 +1047,7 @@ mbq_status launch_lora_backward(const LoraCall& c, hipStream_t stream) {
     f.t = s.t;
     f.fragments = reinterpret_cast<uint4*>(fragments);
     for (int p = 0; p < c.n; ++p) f.h[p] = side ? c.Hin[p] : nullptr;
-    hipLaunchKernelGGL(lora_fragment_kernel, dim3(s.t.tiles, c.n), dim3(64), 0, stream, f);
+    hipLaunchKernelGGL(lora_fragment_kernel, dim3(s.t.tiles, c.n, s.t.rt), dim3(64), 0, stream, f);
     OuterArgs o = {};
     o.t = s.t;
     o.fragments = f.fragments;
