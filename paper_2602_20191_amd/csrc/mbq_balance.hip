@@ -200,11 +200,11 @@ mbq_status launch_balance_loss(const BalanceCall& c, hipStream_t stream) {
 
 // ---- the routers' gradients ----------------------------------------------------------------------------------------
 // One pass over X (and base) for all routers that read it: a lane owns four columns, holds their router weights and their
-// sums of dWr, and walks over the tokens of its share, whose dlogits are scalars.  32 multiply-adds a column and token for
+// sums of dWr, and walks over the tokens of its share, four at a time, whose dlogits come from LDS.  32 multiply-adds a column and token for
 // four routers of four outputs, under half of what the vector units do in the time the memory needs, so it is bound by memory.
 // A workgroup's four wavefronts share 256 columns and take tokens in turn; their sums meet in LDS, the chunks' in a second
 // launch, in order.
-constexpr int kRouteColumns = 256, kRouteWaves = 4, kRouteAhead = 4;  // tokens whose loads are on their way together
+constexpr int kRouteColumns = 256, kRouteWaves = 4, kRouteAhead = 4, kRouteStage = 64;
 
 struct RouteBackwardArgs {
   RouteBackwardCall c;
@@ -218,6 +218,8 @@ template <int kRouters, bool kWide, bool kStream>
 __global__ __launch_bounds__(256) void route_backward_kernel(const RouteBackwardArgs s) {
   constexpr int kOut = kRouters * 4;
   __shared__ float red[kRouteWaves][4][4][64];
+  __shared__ __align__(16) float ds[kRouteStage][kOut];  // dlogits of the tokens at hand, zero for those left out
+  __shared__ uint32_t keeps[kRouteStage];                // all ones, or zero for a token left out
   const RouteBackwardCall& c = s.c;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), P = c.P;
   const int64_t K = c.K, c0 = (int64_t)blockIdx.x * kRouteColumns + (kWide ? 4 * lane : lane);
@@ -232,27 +234,27 @@ __global__ __launch_bounds__(256) void route_backward_kernel(const RouteBackward
       if ((o & 3) < P && column(i) < K) w[o][i] = c.Wr[o >> 2][(int64_t)(o & 3) * K + column(i)];
     }
   const int64_t t0 = (int64_t)blockIdx.y * s.chunk, t1 = min(t0 + s.chunk, c.T);
-  float bias[kOut];  // sums of dlogits, the same in every lane
-#pragma unroll
-  for (int o = 0; o < kOut; ++o) bias[o] = 0.f;
+  float bias = 0.f;  // thread o of the first workgroups: the sum of dlogits of output o
 
-  for (int64_t t = t0 + wave * kRouteAhead; t < t1; t += kRouteWaves * kRouteAhead) {
-    const int count = (int)min((int64_t)kRouteAhead, t1 - t);
+  struct Loads {
     uint2 x[kRouteAhead];
     floatx4 y[kRouteAhead];
+  };
+  const bool with_base = c.dX && c.base;
+  const auto load = [&](Loads& l, int64_t t) {  // tokens t .. t + 3 (those that are not there repeat the last)
 #pragma unroll
     for (int k = 0; k < kRouteAhead; ++k) {
-      const int64_t row = (t + min(k, count - 1)) * K;
-      x[k] = uint2{0, 0};
-      y[k] = floatx4{0.f, 0.f, 0.f, 0.f};
+      const int64_t row = min(t + k, t1 - 1) * K;
+      l.x[k] = uint2{0, 0};
+      l.y[k] = floatx4{0.f, 0.f, 0.f, 0.f};
       if constexpr (kWide) {
         if (c0 < K) {
-          x[k] = *reinterpret_cast<const uint2*>(c.X + row + c0);
-          if (c.dX && c.base) {
+          l.x[k] = *reinterpret_cast<const uint2*>(c.X + row + c0);
+          if (with_base) {
             if constexpr (kStream)
-              y[k] = __builtin_nontemporal_load(reinterpret_cast<const floatx4*>(c.base + row + c0));
+              l.y[k] = __builtin_nontemporal_load(reinterpret_cast<const floatx4*>(c.base + row + c0));
             else
-              y[k] = *reinterpret_cast<const floatx4*>(c.base + row + c0);
+              l.y[k] = *reinterpret_cast<const floatx4*>(c.base + row + c0);
           }
         }
       } else {
@@ -260,25 +262,23 @@ __global__ __launch_bounds__(256) void route_backward_kernel(const RouteBackward
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           v[i] = column(i) < K ? c.X[row + column(i)] : 0;
-          if (c.dX && c.base && column(i) < K) y[k][i] = c.base[row + column(i)];
+          if (with_base && column(i) < K) l.y[k][i] = c.base[row + column(i)];
         }
-        x[k] = uint2{v[0] | v[1] << 16, v[2] | v[3] << 16};
+        l.x[k] = uint2{v[0] | v[1] << 16, v[2] | v[3] << 16};
       }
     }
+  };
+  const auto use = [&](const Loads& l, int64_t t, int at) {  // at: where the tokens' dlogits lie
 #pragma unroll
     for (int k = 0; k < kRouteAhead; ++k) {
-      const int64_t token = t + min(k, count - 1);
-      const bool kept = k < count && (!c.mask || c.mask[token]);  // the same in every lane
-      const uint32_t keep = __builtin_amdgcn_readfirstlane(kept ? 0xFFFFFFFFu : 0u);
+      if (t + k >= t1) break;
+      const uint32_t keep = keeps[at + k];
       float d[kOut];
 #pragma unroll
-      for (int o = 0; o < kOut; ++o) {
-        d[o] = 0.f;
-        if ((o & 3) < P) d[o] = __uint_as_float(__float_as_uint(c.dlogits[o >> 2][token * P + (o & 3)]) & keep);
-        bias[o] += d[o];
-      }
-      const uint32_t xl = x[k].x & keep, xh = x[k].y & keep;
+      for (int o = 0; o < kOut; o += 4) *reinterpret_cast<floatx4*>(d + o) = *reinterpret_cast<const floatx4*>(&ds[at + k][o]);
+      const uint32_t xl = l.x[k].x & keep, xh = l.x[k].y & keep;
       const float xv[4] = {low_bf16(xl), high_bf16(xl), low_bf16(xh), high_bf16(xh)};
+      floatx4 y = l.y[k];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         float g = 0.f;
@@ -287,23 +287,46 @@ __global__ __launch_bounds__(256) void route_backward_kernel(const RouteBackward
           g += d[o] * w[o][i];
           sum[o][i] += d[o] * xv[i];
         }
-        y[k][i] += __uint_as_float(__float_as_uint(g) & keep);
+        y[i] += __uint_as_float(__float_as_uint(g) & keep);
       }
-      if (c.dX && k < count) {
-        float* to = c.dX + token * K;
+      if (c.dX) {
+        float* to = c.dX + (t + k) * K;
         if constexpr (kWide) {
           if (c0 < K) {
             if constexpr (kStream)
-              __builtin_nontemporal_store(y[k], reinterpret_cast<floatx4*>(to + c0));
+              __builtin_nontemporal_store(y, reinterpret_cast<floatx4*>(to + c0));
             else
-              *reinterpret_cast<floatx4*>(to + c0) = y[k];
+              *reinterpret_cast<floatx4*>(to + c0) = y;
           }
         } else {
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            if (column(i) < K) to[column(i)] = y[k][i];
+            if (column(i) < K) to[column(i)] = y[i];
         }
       }
+    }
+  };
+  for (int64_t stage = t0; stage < t1; stage += kRouteStage) {
+    const int count = (int)min((int64_t)kRouteStage, t1 - stage);
+    Loads now, next;
+    if (stage + wave * kRouteAhead < t1) load(now, stage + wave * kRouteAhead);
+    __syncthreads();
+    for (int e = threadIdx.x; e < count * kOut; e += 256) {
+      const int k = e / kOut, o = e - k * kOut;
+      const int64_t token = stage + k;
+      float v = 0.f;
+      if ((o & 3) < P && (!c.mask || c.mask[token])) v = c.dlogits[o >> 2][token * P + (o & 3)];
+      ds[k][o] = v;
+    }
+    for (int k = threadIdx.x; k < count; k += 256) keeps[k] = !c.mask || c.mask[stage + k] ? 0xFFFFFFFFu : 0u;
+    __syncthreads();
+    if (blockIdx.x == 0 && threadIdx.x < kOut)
+      for (int k = 0; k < count; ++k) bias += ds[k][threadIdx.x];
+    for (int k = wave * kRouteAhead; k < count; k += kRouteWaves * kRouteAhead) {
+      const bool more = k + kRouteWaves * kRouteAhead < count;
+      if (more) load(next, stage + k + kRouteWaves * kRouteAhead);
+      use(now, stage + k, k);
+      if (more) now = next;
     }
   }
   const int outputs = kRouters * P;
@@ -326,21 +349,12 @@ __global__ __launch_bounds__(256) void route_backward_kernel(const RouteBackward
         }
       }
     }
-  if (blockIdx.x == 0 && (c.dbr[0] || s.partial)) {
-    __syncthreads();
-    float* const all = &red[0][0][0][0];  // [wave][kOut]
-#pragma unroll
-    for (int o = 0; o < kOut; ++o)
-      if (lane == 0) all[wave * kOut + o] = bias[o];
-    __syncthreads();
+  if (blockIdx.x == 0 && threadIdx.x < kOut && (threadIdx.x & 3) < P && (c.dbr[0] || s.partial)) {
     const int o = threadIdx.x;
-    if (o < kOut && (o & 3) < P) {
-      const float v = (all[o] + all[kOut + o]) + (all[2 * kOut + o] + all[3 * kOut + o]);
-      if (s.partial)
-        s.partial_b[(int64_t)blockIdx.y * outputs + (o >> 2) * P + (o & 3)] = v;
-      else
-        c.dbr[o >> 2][o & 3] = v;
-    }
+    if (s.partial)
+      s.partial_b[(int64_t)blockIdx.y * outputs + (o >> 2) * P + (o & 3)] = bias;
+    else
+      c.dbr[o >> 2][o & 3] = bias;
   }
 }
 
