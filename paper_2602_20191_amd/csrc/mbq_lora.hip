@@ -76,9 +76,9 @@ __device__ __forceinline__ Tile find_tile(const int32_t* __restrict__ offsets, i
 }
 __device__ __forceinline__ int token_at(const int32_t* __restrict__ perm, int T, int i) { return clamped(perm[i], T - 1); }
 // Neighbouring work items on one XCD (blocks go round the eight of them), so that a pool is read into one L2.
-__device__ __forceinline__ int xcd_item(int items) {
+__device__ __forceinline__ int xcd_item(int block, int items) {
   const int per = (items + 7) >> 3;
-  return ((int)blockIdx.x & 7) * per + ((int)blockIdx.x >> 3);
+  return (block >> 3) < per ? (block & 7) * per + (block >> 3) : items;
 }
 unsigned xcd_blocks(int64_t items) { return (unsigned)((items + 7) / 8 * 8); }
 
@@ -302,9 +302,11 @@ __global__ __launch_bounds__(256) void lora_shrink_kernel(const ShrinkArgs s) {
   constexpr int kXBytes = kTile * kXPieces * 16, kWBytes = kUnits * 16 * kWPieces * 16;
   __shared__ __align__(16) char lds[kWaves * (kXBytes + kWBytes)];
   static_assert(sizeof(lds) >= kWaves * kUnits * 8 * 64 * 4, "the sums are joined in the same LDS");
-  const int item = xcd_item(s.t.tiles << s.t.parts_log2);
+  // the tiles of tokens without an adapter come last: where there are many tiles, the others are dealt out evenly
+  const int tiles = s.t.tiles < 64 ? s.t.tiles : clamped(s.t.offsets[s.t.n], s.t.T) / kTile + s.t.n;
+  const int item = xcd_item(blockIdx.x, tiles << s.t.parts_log2);
   const int tile = item >> s.t.parts_log2, part = item & ((1 << s.t.parts_log2) - 1);
-  if (tile >= s.t.tiles) return;
+  if (tile >= tiles) return;
   const int source = blockIdx.y, chunk = blockIdx.z;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = lane >> 4;
   const Tile at = find_tile(s.t.offsets, s.t.n, s.t.T, tile, kTile);
@@ -475,18 +477,22 @@ struct ExpandArgs {
   int64_t L[MBQ_MAX_GROUP];
   int outputs, first[MBQ_MAX_GROUP], blocks;  // blocks of columns: an output's first, of all of them
   int sources;  // projections that add to one output: 1 (forward: the output's own), or all (backward, one output)
+  int steps;    // of 32 ranks of a projection, in by_token
+  const uint4* by_token;
 };
 
-// y = base + sum over the sources of scale h w for a tile.  h, cut into pieces, goes through LDS 32 ranks at a time (lane:
-// token, eight ranks); w is turned in registers: a lane loads four columns of eight ranks and pairs ranks up by one byte
+// y = base + sum over the sources of scale h w for a tile.  h goes 32 ranks at a time (lane: token, eight ranks): cut into
+// pieces through LDS, or (kCut) as lora_fragment_kernel left it; w is turned in registers: a lane loads four columns of eight ranks and pairs ranks up by one byte
 // permutation a dword.  kWide: MFMA c of a set of four yields columns 4 (lane mod 16) + c, so that a lane's four results of
 // one token are one 16-byte access to base and y; else columns 16 c + lane mod 16.  base, and the next step's h and w, are on
 // their way while a step is multiplied.  Bound by reading base and writing y.
-template <bool kWide, bool kStream>
-__global__ __launch_bounds__(256) void lora_expand_kernel(const ExpandArgs s) {
-  constexpr int kStep = 32, kStride = kStep + 8;
-  __shared__ __align__(16) uint16_t pieces[2][3][kTile][kStride];
-  const int item = xcd_item(s.t.tiles * s.blocks);
+constexpr int kStep = 32, kStride = kStep + 8;
+struct ExpandLds {
+  uint16_t pieces[2][3][kTile][kStride];
+};
+template <bool kWide, bool kStream, bool kCut>
+__device__ __forceinline__ void expand_block(const ExpandArgs& s, int block_id, ExpandLds* lds) {
+  const int item = xcd_item(block_id, s.t.tiles * s.blocks);
   if (item >= s.t.tiles * s.blocks) return;
   const int tile = item / s.blocks;
   int block = item - tile * s.blocks, out = 0;
@@ -540,11 +546,18 @@ __global__ __launch_bounds__(256) void lora_expand_kernel(const ExpandArgs s) {
   // steps of 32 ranks, source by source
   const int p0 = s.sources == 1 ? out : 0, per = (own + kStep - 1) / kStep, steps = per * s.sources;
   float4 hv;
+  uint4 hf[kCut ? 6 : 1];
   uint2 wv[8];  // four columns of ranks 8 q ..
   const auto load = [&](int p, int j0) {
-    const int j = j0 + 4 * (tid & 7);
-    hv = float4{0.f, 0.f, 0.f, 0.f};
-    if (j < own) hv = whole_h(s.t, p, place, j);
+    if constexpr (kCut) {
+      const uint4* from = s.by_token + (((int64_t)tile * s.sources + p) * s.steps + j0 / kStep) * 384 + lane;
+#pragma unroll
+      for (int i = 0; i < 6; ++i) hf[i] = from[64 * i];
+    } else {
+      const int j = j0 + 4 * (tid & 7);
+      hv = float4{0.f, 0.f, 0.f, 0.f};
+      if (j < own) hv = whole_h(s.t, p, place, j);
+    }
     const uint16_t* w = s.w[p] + (int64_t)at.a * s.t.r * L;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {  // ranks that are not there meet zeros
@@ -560,7 +573,11 @@ __global__ __launch_bounds__(256) void lora_expand_kernel(const ExpandArgs s) {
   if (steps) load(p0, 0);
   int p = p0, j0 = 0;
   for (int step = 0; step < steps; ++step) {
-    {
+    uint4 a[kCut ? 6 : 1];
+    if constexpr (kCut) {
+#pragma unroll
+      for (int i = 0; i < 6; ++i) a[i] = hf[i];
+    } else {
       const int j = j0 + 4 * (tid & 7);
       float v[4] = {hv.x, hv.y, hv.z, hv.w};
 #pragma unroll
@@ -574,7 +591,7 @@ __global__ __launch_bounds__(256) void lora_expand_kernel(const ExpandArgs s) {
       cut_pair(v[0], v[1], pc[2].x, pc[1].x, pc[0].x);
       cut_pair(v[2], v[3], pc[2].y, pc[1].y, pc[0].y);
 #pragma unroll
-      for (int i = 0; i < 3; ++i) *reinterpret_cast<uint2*>(&pieces[step & 1][i][tid >> 3][4 * (tid & 7)]) = pc[i];
+      for (int i = 0; i < 3; ++i) *reinterpret_cast<uint2*>(&lds->pieces[step & 1][i][tid >> 3][4 * (tid & 7)]) = pc[i];
     }
     uint4 w4[4];
 #pragma unroll
@@ -590,14 +607,18 @@ __global__ __launch_bounds__(256) void lora_expand_kernel(const ExpandArgs s) {
     j0 += kStep;
     if (j0 >= own) ++p, j0 = 0;
     if (step + 1 < steps) load(p, j0);
-    __syncthreads();  // (the other buffer's readers passed the barrier before: two buffers do)
+    if constexpr (!kCut) __syncthreads();  // (the other buffer's readers passed the barrier before: two buffers do)
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int i = 0; i < 3; ++i)
 #pragma unroll
-      for (int i = 0; i < 3; ++i) {
-        const uint4 a = *reinterpret_cast<const uint4*>(&pieces[step & 1][i][16 * h + (lane & 15)][8 * q]);
+      for (int h = 0; h < 2; ++h) {
+        uint4 av;
+        if constexpr (kCut)
+          av = a[2 * i + h];
+        else
+          av = *reinterpret_cast<const uint4*>(&lds->pieces[step & 1][i][16 * h + (lane & 15)][8 * q]);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) acc[h][c] = bf::mfma(a, w4[c], acc[h][c]);
+        for (int c = 0; c < 4; ++c) acc[h][c] = bf::mfma(av, w4[c], acc[h][c]);
       }
   }
   if (H)  // ranks that are not there
@@ -623,43 +644,85 @@ __global__ __launch_bounds__(256) void lora_expand_kernel(const ExpandArgs s) {
     }
 }
 
-// The operands of the gradients' products over tokens: fragments[projection][tile][unit of the projection][piece][lane] holds
-// 16 bytes, rank 16 unit + lane mod 16 of tokens 8 (lane / 16) .. + 7 of the tile; tokens that are not there are zero.  One
-// wavefront per (tile, projection, unit): of g (summed over its parts) or of h as the forward pass left it, times the scale.
+template <bool kWide, bool kStream>
+__global__ __launch_bounds__(256) void lora_expand_kernel(const ExpandArgs s) {
+  __shared__ __align__(16) ExpandLds lds;
+  expand_block<kWide, kStream, false>(s, blockIdx.x, &lds);
+}
+
+// The operands of the gradients' products, cut into pieces and scaled.  By ranks, for the products over tokens:
+// fragments[projection][tile][unit][piece][lane] holds 16 bytes, rank 16 unit + lane mod 16 of tokens 8 (lane / 16) .. + 7 of
+// the tile.  By tokens, for dX: by_token[tile][projection][32 ranks][piece][half][lane], token 16 half + lane mod 16, ranks
+// 8 (lane / 16) .. + 7.  What is not there is zero.  One wavefront per (tile, projection, 32 ranks), of g (summed over its
+// parts) and of h as the forward pass left it.
 struct FragmentArgs {
   TileArgs t;
-  const float* h[MBQ_MAX_GROUP];  // null: g from t.partial
-  uint4* fragments;
+  int n, steps;  // projections; 32 ranks each
+  const float* h[MBQ_MAX_GROUP];
+  uint4 *g_fragments, *h_fragments, *by_token;  // null: not wanted
 };
 __global__ __launch_bounds__(64) void lora_fragment_kernel(const FragmentArgs s) {
-  const int tile = blockIdx.x, p = blockIdx.y, unit = blockIdx.z, lane = threadIdx.x, q = lane >> 4;
+  constexpr int kStride = 36;  // floats: 16-byte rows in LDS, spread over the banks
+  __shared__ __align__(16) float v[kTile][kStride];  // [token][rank]
+  const int tile = blockIdx.x, p = blockIdx.y, step = blockIdx.z >> 1, lane = threadIdx.x, q = lane >> 4;
+  const bool of_h = blockIdx.z & 1;
+  if (of_h ? !s.h_fragments : !s.g_fragments && !s.by_token) return;
   const Tile at = find_tile(s.t.offsets, s.t.n, s.t.T, tile, kTile);
   if (at.a >= s.t.n || at.count == 0) return;
   const int own = own_rank(s.t.ranks, at.a, s.t.r);
   const float scale = s.t.scale[at.a];
-  {
-    const int j = 16 * unit + (lane & 15);
-    float v[8] = {};
-    if (j < own) {
-      if (s.h[p]) {
+  // lane: rank j, every other token
+  const int j = 32 * step + (lane & 31);
+  float sum[kTile / 2];
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          v[e] = s.h[p][(int64_t)token_at(s.t.perm, s.t.T, at.begin + min(8 * q + e, at.count - 1)) * s.t.r + j];
-      } else {
-        const float* from = s.t.partial + ((int64_t)(p * s.t.rt + unit) * s.t.T + at.begin) * 16 + (lane & 15);
-        for (int i = 0; i < 1 << s.t.parts_log2; ++i, from += (int64_t)s.t.units * s.t.T * 16)
+  for (int e = 0; e < kTile / 2; ++e) sum[e] = 0.f;
+  if (j < own) {
+    if (of_h) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] += from[min(8 * q + e, at.count - 1) * 16];
+      for (int e = 0; e < kTile / 2; ++e) {
+        const int place = at.begin + min(2 * e + (lane >> 5), at.count - 1);
+        sum[e] = s.h[p][(int64_t)token_at(s.t.perm, s.t.T, place) * s.t.r + j];
       }
+    } else {
+      const float* from = s.t.partial + ((int64_t)(p * s.t.rt + (j >> 4)) * s.t.T + at.begin) * 16 + (j & 15);
+      for (int i = 0; i < 1 << s.t.parts_log2; ++i, from += (int64_t)s.t.units * s.t.T * 16)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = 8 * q + e < at.count ? v[e] * scale : 0.f;
+        for (int e = 0; e < kTile / 2; ++e) sum[e] += from[min(2 * e + (lane >> 5), at.count - 1) * 16];
     }
-    const Pieces pc = cut(v);
-    uint4* to = s.fragments + (((int64_t)p * s.t.tiles + tile) * s.t.rt + unit) * 192 + lane;
-    to[0] = pc.hi;
-    to[64] = pc.mid;
-    to[128] = pc.lo;
   }
+#pragma unroll
+  for (int e = 0; e < kTile / 2; ++e) {
+    const int token = 2 * e + (lane >> 5);
+    v[token][lane & 31] = j < own && token < at.count ? sum[e] * scale : 0.f;
+  }
+  __syncthreads();
+  uint4* const fragments = of_h ? s.h_fragments : s.g_fragments;
+  if (fragments)
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int unit = 2 * step + u;
+      if (unit >= s.t.rt) continue;
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = v[8 * q + e][16 * u + (lane & 15)];
+      const Pieces pc = cut(x);
+      uint4* to = fragments + (((int64_t)p * s.t.tiles + tile) * s.t.rt + unit) * 192 + lane;
+      to[0] = pc.hi;
+      to[64] = pc.mid;
+      to[128] = pc.lo;
+    }
+  if (!of_h && s.by_token)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = v[16 * h + (lane & 15)][8 * q + e];
+      const Pieces pc = cut(x);
+      uint4* to = s.by_token + (((int64_t)tile * s.n + p) * s.steps + step) * 384 + h * 64 + lane;
+      to[0] = pc.lo;
+      to[128] = pc.mid;
+      to[256] = pc.hi;
+    }
 }
 
 struct OuterArgs {
@@ -670,109 +733,255 @@ struct OuterArgs {
   float* d[MBQ_MAX_GROUP];
   float* more[MBQ_MAX_GROUP];  // [chunk][r][L]: chunks of an adapter behind its first
   int chunk;                   // tokens of a chunk, a multiple of kTile * kWaves
-  int groups;                  // of kUnits units; grid.y = groups * projections
+  int chunks;                  // of all adapters
+  int groups;                  // of kUnits units
   int blocks;                  // of columns, of the widest
+  int round;                   // workgroups of a (projection, group)
 };
+struct OuterWork {
+  Tile at;
+  int p, unit0, units, block, tile0;  // tile0: the chunk's first tile among all
+  float* d;                           // an adapter's first chunk goes to the gradient itself
+};
+template <int kUnits, int kWidth>
+__device__ __forceinline__ bool outer_work(const OuterArgs& s, int block_id, OuterWork& w) {
+  const int of = block_id / s.round, item = xcd_item(block_id - of * s.round, s.chunks * s.blocks);
+  if (item >= s.chunks * s.blocks) return false;
+  // an XCD has a range of columns and all chunks, some of which are empty; a tile's h is small
+  w.block = item / s.chunks;
+  const int number = item - w.block * s.chunks;
+  w.p = of / s.groups;
+  w.unit0 = (of - w.p * s.groups) * kUnits;
+  w.units = min(kUnits, s.t.rt - w.unit0);
+  const int64_t L = s.L[w.p];
+  if ((int64_t)w.block * kWidth >= L) return false;
+  w.at = find_tile(s.t.offsets, s.t.n, s.t.T, number, s.chunk);
+  if (w.at.a >= s.t.n || (w.at.count == 0 && w.at.first > 0)) return false;
+  const int off = clamped(s.t.offsets[w.at.a], s.t.T);
+  w.tile0 = off / kTile + w.at.a + w.at.first * (s.chunk / kTile);
+  w.d = w.at.first == 0 ? s.d[w.p] + (int64_t)w.at.a * s.t.r * L
+                        : s.more[w.p] + (int64_t)(off / s.chunk + w.at.first) * s.t.r * L;
+  if (own_rank(s.t.ranks, w.at.a, s.t.r) <= 16 * w.unit0) w.at.count = 0;  // zeros
+  return true;
+}
+// The tokens of a lane's eight rows of a tile.
+struct Rows {
+  int token[8];
+};
+__device__ __forceinline__ Rows rows_of(const TileArgs& t, const Tile& at, int i) {
+  Rows r;
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    r.token[e] = token_at(t.perm, t.T, at.begin + min(i * kTile + 8 * ((int)(threadIdx.x & 63) >> 4) + e, at.count - 1));
+  return r;
+}
 
-// Chunk of d[a] = h^T x over the tokens of a chunk: ranks are the rows, x is turned in registers: a lane loads 16 bytes of
-// eight tokens' rows, and a dword of MFMA c's operand pairs two tokens of column c (for bf16 one byte permutation; fp32 values
-// are cut into pieces, and of the nine products of pieces the six above 2^-32 are formed).  Four wavefronts take tiles in
-// turn and are added in LDS.  An adapter's first chunk goes to d itself.  Bound by reading x.
-template <typename In, int kUnits, bool kWide>
-__global__ __launch_bounds__(256) void lora_outer_kernel(const OuterArgs s) {
-  constexpr int kCols = 16 / (int)sizeof(In), kWidth = 16 * kCols;  // columns of a lane, of the workgroup
-  __shared__ float red[kWaves][kCols * 4][64];
-  const int chunks = s.t.T / s.chunk + s.t.n + 1;
-  const int item = xcd_item(chunks * s.blocks);
-  if (item >= chunks * s.blocks) return;
-  const int number = item / s.blocks, block = item - number * s.blocks;
-  const int p = blockIdx.y / s.groups, unit0 = (blockIdx.y - p * s.groups) * kUnits;
-  const int64_t L = s.L[p];
-  if ((int64_t)block * kWidth >= L) return;
-  const Tile at = find_tile(s.t.offsets, s.t.n, s.t.T, number, s.chunk);
-  if (at.a >= s.t.n || (at.count == 0 && at.first > 0)) return;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, q = lane >> 4;
-  const int64_t c = (int64_t)block * kWidth + (lane & 15) * kCols;
-  const In* x = static_cast<const In*>(s.x[p]);
-  // the chunk's first tile among all tiles
-  const int off = clamped(s.t.offsets[at.a], s.t.T), tile0 = off / kTile + at.a + at.first * (s.chunk / kTile);
-  const int units = min(kUnits, s.t.rt - unit0);
-  floatx4 acc[kUnits][kCols];
+// dA[a] = g^T x over a chunk's tokens: ranks are the rows, x is turned in registers: a lane loads eight columns of eight tokens'
+// rows, and one byte permutation a dword pairs two tokens of a column.  128 columns a workgroup; its four wavefronts take
+// tiles in turn, the next tile's x under way, and are added in LDS.
+constexpr int kWidthX = 128, kWidthY = 256;  // columns of a workgroup
+struct OuterXLds {
+  float red[kWaves][32][64];
+};
+template <int kUnits>
+__device__ __forceinline__ void outer_x_block(const OuterArgs& s, int block_id, OuterXLds* lds) {
+  constexpr int kWidth = kWidthX;
+  auto& red = lds->red;
+  OuterWork w;
+  if (!outer_work<kUnits, kWidth>(s, block_id, w)) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t L = s.L[w.p], c = (int64_t)w.block * kWidth + (lane & 15) * 8;  // (K is a multiple of 128)
+  const uint16_t* x = static_cast<const uint16_t*>(s.x[w.p]) + c;
+  floatx4 acc[kUnits][8];
 #pragma unroll
   for (int u = 0; u < kUnits; ++u)
 #pragma unroll
-    for (int e = 0; e < kCols; ++e) acc[u][e] = floatx4{0.f, 0.f, 0.f, 0.f};
-
-  if (own_rank(s.t.ranks, at.a, s.t.r) > 16 * unit0)
-    for (int i = wave; i * kTile < at.count; i += kWaves) {
-      const uint4* from = s.fragments + (((int64_t)p * s.t.tiles + tile0 + i) * s.t.rt + unit0) * 192 + lane;
-      uint4 h[kUnits][3];
+    for (int e = 0; e < 8; ++e) acc[u][e] = floatx4{0.f, 0.f, 0.f, 0.f};
+  uint4 v[8], h[kUnits][3];
+  const auto load = [&](int i, const Rows& r) {
+    const uint4* from = s.fragments + (((int64_t)w.p * s.t.tiles + w.tile0 + i) * s.t.rt + w.unit0) * 192 + lane;
 #pragma unroll
-      for (int u = 0; u < kUnits; ++u)
+    for (int e = 0; e < 8; ++e) v[e] = *reinterpret_cast<const uint4*>(x + (int64_t)r.token[e] * L);
 #pragma unroll
-        for (int k = 0; k < 3; ++k) h[u][k] = from[(u < units ? u : 0) * 192 + k * 64];
-      uint4 v[8];
+    for (int u = 0; u < kUnits; ++u)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const In* row = x + (int64_t)token_at(s.t.perm, s.t.T, at.begin + min(i * kTile + 8 * q + e, at.count - 1)) * L;
-        if constexpr (kWide) {
-          v[e] = *reinterpret_cast<const uint4*>(row + min(c, L - kCols));
-        } else if constexpr (sizeof(In) == 4) {
-          const uint32_t* bits = reinterpret_cast<const uint32_t*>(row);
-          v[e] = uint4{bits[min(c, L - 1)], bits[min(c + 1, L - 1)], bits[min(c + 2, L - 1)], bits[min(c + 3, L - 1)]};
-        }
-      }
+      for (int k = 0; k < 3; ++k) h[u][k] = from[(u < w.units ? u : 0) * 192 + k * 64];
+  };
+  const int tiles = (w.at.count + kTile - 1) / kTile;
+  Rows r;
+  if (wave < tiles) {
+    r = rows_of(s.t, w.at, wave);
+    load(wave, r);
+    if (wave + kWaves < tiles) r = rows_of(s.t, w.at, wave + kWaves);
+  }
+  for (int i = wave; i < tiles; i += kWaves) {
+    uint4 xv[8], hv[kUnits][3];
 #pragma unroll
-      for (int col = 0; col < kCols; ++col) {
-        const auto word = [&](int e) {
-          const int k = sizeof(In) == 2 ? col >> 1 : col;
-          return k == 0 ? v[e].x : k == 1 ? v[e].y : k == 2 ? v[e].z : v[e].w;
-        };
-        if constexpr (sizeof(In) == 2) {
-          uint32_t d[4];
+    for (int col = 0; col < 8; ++col) {
+      const auto word = [&](int e) { return col < 2 ? v[e].x : col < 4 ? v[e].y : col < 6 ? v[e].z : v[e].w; };
+      uint32_t d[4];
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            d[e] = __builtin_amdgcn_perm(word(2 * e + 1), word(2 * e), col & 1 ? 0x07060302u : 0x05040100u);
-          const uint4 xv = {d[0], d[1], d[2], d[3]};
-#pragma unroll
-          for (int u = 0; u < kUnits; ++u)
-#pragma unroll
-            for (int k = 2; k >= 0; --k) acc[u][col] = bf::mfma(h[u][k], xv, acc[u][col]);
-        } else {
-          float f[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(word(e));
-          const Pieces pc = cut(f);
-#pragma unroll
-          for (int u = 0; u < kUnits; ++u) {
-            acc[u][col] = bf::mfma(h[u][2], pc.hi, acc[u][col]);
-            acc[u][col] = bf::mfma(h[u][1], pc.mid, acc[u][col]);
-            acc[u][col] = bf::mfma(h[u][0], pc.lo, acc[u][col]);
-            acc[u][col] = bf::mfma(h[u][1], pc.hi, acc[u][col]);
-            acc[u][col] = bf::mfma(h[u][0], pc.mid, acc[u][col]);
-            acc[u][col] = bf::mfma(h[u][0], pc.hi, acc[u][col]);
-          }
-        }
-      }
+      for (int e = 0; e < 4; ++e)
+        d[e] = __builtin_amdgcn_perm(word(2 * e + 1), word(2 * e), col & 1 ? 0x07060302u : 0x05040100u);
+      xv[col] = uint4{d[0], d[1], d[2], d[3]};
     }
-  float* d = at.first == 0 ? s.d[p] + (int64_t)at.a * s.t.r * L
-                           : s.more[p] + (int64_t)(off / s.chunk + at.first) * s.t.r * L;
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u)
+#pragma unroll
+      for (int k = 0; k < 3; ++k) hv[u][k] = h[u][k];
+    if (i + kWaves < tiles) {
+      load(i + kWaves, r);
+      if (i + 2 * kWaves < tiles) r = rows_of(s.t, w.at, i + 2 * kWaves);
+    }
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u)
+#pragma unroll
+      for (int k = 2; k >= 0; --k)
+#pragma unroll
+        for (int col = 0; col < 8; ++col) acc[u][col] = bf::mfma(hv[u][k], xv[col], acc[u][col]);
+  }
 #pragma unroll
   for (int u = 0; u < kUnits; ++u) {
     if (u) __syncthreads();
 #pragma unroll
-    for (int e = 0; e < kCols; ++e)
+    for (int e = 0; e < 8; ++e)
 #pragma unroll
       for (int i = 0; i < 4; ++i) red[wave][e * 4 + i][lane] = acc[u][e][i];
     __syncthreads();
     for (int e = tid; e < 16 * kWidth; e += 256) {
-      const int j = e / kWidth, col = e - j * kWidth, value = (col % kCols) * 4 + (j & 3), l = (j >> 2) * 16 + col / kCols;
-      const int64_t to = (int64_t)block * kWidth + col;
-      if (u < units && 16 * (unit0 + u) + j < s.t.r && to < L)
-        d[(int64_t)(16 * (unit0 + u) + j) * L + to] =
+      const int j = e / kWidth, col = e - j * kWidth, value = (col & 7) * 4 + (j & 3), l = (j >> 2) * 16 + (col >> 3);
+      if (u < w.units && 16 * (w.unit0 + u) + j < s.t.r)
+        w.d[(int64_t)(16 * (w.unit0 + u) + j) * L + (int64_t)w.block * kWidth + col] =
             (red[0][value][l] + red[1][value][l]) + (red[2][value][l] + red[3][value][l]);
     }
   }
+}
+
+// dB[a] = h^T dy over a chunk's tokens, the same way: a lane loads four columns of eight tokens' rows, cuts the values into
+// pieces as it pairs tokens up, and of the nine products of pieces the six above 2^-32 are formed.  256 columns a workgroup,
+// 64 a wavefront, tile after tile; a tile's h is shared through LDS, the next tile's h and dy are under way.
+// kWide: columns 4 (lane mod 16) + c, 16-byte accesses; else 16 c + lane mod 16.
+template <int kUnits>
+struct OuterYLds {
+  uint4 hs[2][kUnits * 192];
+};
+template <int kUnits, bool kWide>
+__device__ __forceinline__ void outer_y_block(const OuterArgs& s, int block_id, OuterYLds<kUnits>* lds) {
+  constexpr int kWidth = kWidthY, kLoads = (kUnits * 192 + 255) / 256;
+  OuterWork w;
+  if (!outer_work<kUnits, kWidth>(s, block_id, w)) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, q = lane >> 4;
+  const int64_t L = s.L[w.p], c0 = (int64_t)w.block * kWidth + wave * 64 + (lane & 15) * (kWide ? 4 : 1);
+  const auto column = [&](int c) { return c0 + (kWide ? c : 16 * c); };
+  const float* x = static_cast<const float*>(s.x[w.p]);
+  floatx4 acc[kUnits][4];
+#pragma unroll
+  for (int u = 0; u < kUnits; ++u)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[u][e] = floatx4{0.f, 0.f, 0.f, 0.f};
+  struct Loads {
+    floatx4 v[8];
+    uint4 h[kLoads];
+  };
+  const int tiles = (w.at.count + kTile - 1) / kTile;
+  const uint4* const fragments = s.fragments + (((int64_t)w.p * s.t.tiles + w.tile0) * s.t.rt + w.unit0) * 192;
+  Rows r;
+  // tile i, whose tokens are in r; then the tokens of the next
+  const auto load = [&](Loads& l, int i) {
+    if (i >= tiles) return;
+    const uint4* from = fragments + (int64_t)i * s.t.rt * 192;
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k) {
+      const int e = tid + 256 * k;
+      l.h[k] = from[e < w.units * 192 ? e : 0];  // (units that are not there are not written)
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float* row = x + (int64_t)r.token[e] * L;
+      if constexpr (kWide) {
+        l.v[e] = *reinterpret_cast<const floatx4*>(row + min(c0, L - 4));
+      } else {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) l.v[e][c] = row[min(column(c), L - 1)];
+      }
+    }
+    if (i + 1 < tiles) r = rows_of(s.t, w.at, i + 1);
+  };
+  const auto use = [&](Loads& l, int i) {
+    auto& hs = lds->hs[i & 1];
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k)
+      if (tid + 256 * k < kUnits * 192) hs[tid + 256 * k] = l.h[k];
+    Pieces pc[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const float f[8] = {l.v[0][c], l.v[1][c], l.v[2][c], l.v[3][c], l.v[4][c], l.v[5][c], l.v[6][c], l.v[7][c]};
+      pc[c] = cut(f);
+    }
+    load(l, i + 2);
+    __syncthreads();  // (the other buffer's readers passed the barrier before: two buffers do)
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+      const uint4 hi = hs[u * 192 + lane], mid = hs[u * 192 + 64 + lane], lo = hs[u * 192 + 128 + lane];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) acc[u][c] = bf::mfma(lo, pc[c].hi, acc[u][c]);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) acc[u][c] = bf::mfma(mid, pc[c].mid, acc[u][c]);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) acc[u][c] = bf::mfma(hi, pc[c].lo, acc[u][c]);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) acc[u][c] = bf::mfma(mid, pc[c].hi, acc[u][c]);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) acc[u][c] = bf::mfma(hi, pc[c].mid, acc[u][c]);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) acc[u][c] = bf::mfma(hi, pc[c].hi, acc[u][c]);
+    }
+  };
+  Loads a, b;
+  if (tiles) r = rows_of(s.t, w.at, 0);
+  load(a, 0);
+  load(b, 1);
+  for (int i = 0; i < tiles; i += 2) {
+    use(a, i);
+    if (i + 1 < tiles) use(b, i + 1);
+  }
+#pragma unroll
+  for (int u = 0; u < kUnits; ++u) {
+    if (u >= w.units) continue;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int j = 16 * (w.unit0 + u) + 4 * q + i;
+      if (j >= s.t.r) continue;
+      float* to = w.d + (int64_t)j * L;
+      const floatx4 value = {acc[u][0][i], acc[u][1][i], acc[u][2][i], acc[u][3][i]};
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        if (column(c) < L) to[column(c)] = value[c];
+    }
+  }
+}
+
+// What comes after g and h are cut: dB, dA and dX in one launch, the longest first.  Each alone leaves much of the chip
+// waiting for its own loads.
+struct GradientArgs {
+  OuterArgs y, x;
+  ExpandArgs dx;
+  int y_blocks, x_blocks;  // workgroups of dB, of dA; the others do dX
+};
+template <int kUnits, bool kWideY, bool kWideX, bool kStream>
+__global__ __launch_bounds__(256, 2) void lora_gradient_kernel(const GradientArgs s) {
+  constexpr int kUnitsX = kUnits < 2 ? kUnits : 2;
+  __shared__ __align__(16) union {
+    OuterYLds<kUnits> y;
+    OuterXLds x;
+  } lds;
+  const int block = blockIdx.x;
+  if (block < s.y_blocks)
+    outer_y_block<kUnits, kWideY>(s.y, block, &lds.y);
+  else if (block < s.y_blocks + s.x_blocks)
+    outer_x_block<kUnitsX>(s.x, block - s.y_blocks, &lds.x);
+  else
+    expand_block<kWideX, kStream, true>(s.dx, block - s.y_blocks - s.x_blocks, nullptr);
 }
 
 // d[a] += the chunks behind an adapter's first, in order.
@@ -792,9 +1001,18 @@ __global__ __launch_bounds__(256) void lora_join_kernel(const JoinArgs s) {
   if (chunks == 0) return;
   const int64_t values = s.values[k];
   float* d = s.d[k];
+  const float* more = s.more[k] + (int64_t)(off / chunk) * values;
   for (int64_t i = (int64_t)blockIdx.y * 256 + threadIdx.x; i < values; i += (int64_t)gridDim.y * 256) {
     float sum = d[a * values + i];
-    for (int c = 1; c <= chunks; ++c) sum += s.more[k][(int64_t)(off / chunk + c) * values + i];
+    int c = 1;
+    for (; c + 3 <= chunks; c += 4) {
+      float v[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = more[(c + e) * values + i];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum += v[e];
+    }
+    for (; c <= chunks; ++c) sum += more[c * values + i];
     d[a * values + i] = sum;
   }
 }
@@ -854,65 +1072,66 @@ void shrink(const ShrinkArgs& s, int sources, hipStream_t stream) {
     hipLaunchKernelGGL((lora_shrink_kernel<In, 4, kWide>), grid, dim3(256), 0, stream, s);
 }
 
-void expand(const ExpandArgs& s0, int outputs, bool w, hipStream_t stream) {
-  ExpandArgs s = s0;
-  int64_t columns = 0;
-  s.outputs = outputs;
+// -> workgroups
+int64_t expand_blocks(ExpandArgs* s, int outputs) {
+  s->outputs = outputs;
   for (int i = 0; i < outputs; ++i) {
-    s.first[i] = s.blocks;
-    s.blocks += (int)(up(s.L[i], kExpandColumns) / kExpandColumns);
-    columns += s.L[i];
+    s->first[i] = s->blocks;
+    s->blocks += (int)(up(s->L[i], kExpandColumns) / kExpandColumns);
   }
-  const dim3 grid(xcd_blocks((int64_t)s.t.tiles * s.blocks));
-  if (!w)
-    hipLaunchKernelGGL((lora_expand_kernel<false, false>), grid, dim3(256), 0, stream, s);
-  else if (s.t.T * columns * 4 > kCacheBytes)
-    hipLaunchKernelGGL((lora_expand_kernel<true, true>), grid, dim3(256), 0, stream, s);
-  else
-    hipLaunchKernelGGL((lora_expand_kernel<true, false>), grid, dim3(256), 0, stream, s);
+  return xcd_blocks((int64_t)s->t.tiles * s->blocks);
 }
+bool streams_past(int64_t T, int64_t columns) { return T * columns * 4 > kCacheBytes; }
 
-template <typename In, bool kWide>
-void outer(const OuterArgs& s, int n, hipStream_t stream) {
-  const dim3 grid(xcd_blocks((int64_t)(s.t.T / s.chunk + s.t.n + 1) * s.blocks), (unsigned)(n * s.groups));
-  if (s.t.rt == 1)
-    hipLaunchKernelGGL((lora_outer_kernel<In, 1, kWide>), grid, dim3(256), 0, stream, s);
-  else if (s.t.rt == 2)
-    hipLaunchKernelGGL((lora_outer_kernel<In, 2, kWide>), grid, dim3(256), 0, stream, s);
+constexpr int kUnitsX = 2, kUnitsY = 4;  // of the kernels above at the largest ranks
+template <int kUnits>
+void gradients(const GradientArgs& g, bool wy, bool wx, bool streams, unsigned blocks, hipStream_t stream) {
+  const dim3 grid(blocks), threads(256);
+  if (wy && wx && streams)
+    hipLaunchKernelGGL((lora_gradient_kernel<kUnits, true, true, true>), grid, threads, 0, stream, g);
+  else if (wy && wx)
+    hipLaunchKernelGGL((lora_gradient_kernel<kUnits, true, true, false>), grid, threads, 0, stream, g);
+  else if (wy)
+    hipLaunchKernelGGL((lora_gradient_kernel<kUnits, true, false, false>), grid, threads, 0, stream, g);
+  else if (wx)
+    hipLaunchKernelGGL((lora_gradient_kernel<kUnits, false, true, false>), grid, threads, 0, stream, g);
   else
-    hipLaunchKernelGGL((lora_outer_kernel<In, 4, kWide>), grid, dim3(256), 0, stream, s);
+    hipLaunchKernelGGL((lora_gradient_kernel<kUnits, false, false, false>), grid, threads, 0, stream, g);
 }
+int outer_groups(int rt, int units) { return (rt + units - 1) / units; }
 
-// Tokens of a chunk of the gradients' products: about 1024 workgroups, but chunks of at least 8 r tokens, whose arrays are
-// then small beside what a chunk reads.
+// Tokens of a chunk of the gradients' products: about two workgroups a compute unit, but chunks of at least 8 r tokens, whose
+// arrays are then small beside what a chunk reads.
 int outer_chunk(int64_t T, int64_t workgroups, int r) {
-  int64_t chunk = T * workgroups / 1024;
+  int64_t chunk = T * workgroups / 512;
   if (chunk < 8 * r) chunk = 8 * r;
+  if (chunk > T) chunk = T;
   return (int)up(chunk < 1 ? 1 : chunk, kTile * kWaves);
 }
 int64_t blocks_of(int64_t L, int width) { return up(L, width) / width; }
-constexpr int kWidthX = 128, kWidthY = 64;  // columns of a workgroup of lora_outer_kernel: bf16, fp32
 
 struct BackwardPlan {
   int parts_log2, chunk_x, chunk_y;
-  size_t partial, fragments, more_x, more_y[MBQ_MAX_GROUP];  // bytes; fragments: of g or of h
+  size_t partial, fragments, by_token, more_x, more_y[MBQ_MAX_GROUP];  // bytes; fragments: of g or of h
   size_t bytes;
 };
 BackwardPlan backward_plan(int64_t T, int64_t K, int n, const int64_t* N, int64_t adapters, int r) {
   BackwardPlan b = {};
-  const int rt = (r + 15) / 16, groups = (rt + 3) / 4;
+  const int rt = (r + 15) / 16;
   int64_t most = 0, blocks = 0;
   for (int p = 0; p < n; ++p) {
     most = N[p] > most ? N[p] : most;
     blocks += blocks_of(N[p], kWidthY);
   }
   b.parts_log2 = shrink_parts_log2(T, most);
-  b.chunk_x = outer_chunk(T, blocks_of(K, kWidthX) * n * groups, r);
-  b.chunk_y = outer_chunk(T, blocks * groups, r);
+  b.chunk_x = outer_chunk(T, blocks_of(K, kWidthX) * n * outer_groups(rt, kUnitsX), r);
+  b.chunk_y = outer_chunk(T, blocks * outer_groups(rt, kUnitsY), r);
+  const int64_t tiles = T / kTile + adapters + 1;
   b.partial = up((int64_t)partial_bytes(T, rt * n, b.parts_log2), 256);
-  b.fragments = (size_t)n * (T / kTile + adapters + 1) * rt * 3072;
+  b.fragments = (size_t)n * tiles * rt * 3072;
+  b.by_token = (size_t)n * tiles * ((r + 31) / 32) * 6144;
   b.more_x = up((int64_t)((T - 1) / b.chunk_x + 1) * r * K * 4, 256);
-  b.bytes = b.partial + 2 * b.fragments;
+  b.bytes = b.partial + 2 * b.fragments + b.by_token;
   for (int p = 0; p < n; ++p) {
     b.more_y[p] = up((int64_t)((T - 1) / b.chunk_y + 1) * r * N[p] * 4, 256);
     b.bytes += (T > b.chunk_x ? b.more_x : 0) + (T > b.chunk_y ? b.more_y[p] : 0);
@@ -984,7 +1203,15 @@ mbq_status launch_lora(const LoraCall& c, hipStream_t stream) {
   shrink<uint16_t, true>(s, 1, stream);
   e.t = s.t;
   e.sources = 1;
-  expand(e, c.n, w, stream);
+  const dim3 grid((unsigned)expand_blocks(&e, c.n));
+  int64_t columns = 0;
+  for (int p = 0; p < c.n; ++p) columns += c.N[p];
+  if (!w)
+    hipLaunchKernelGGL((lora_expand_kernel<false, false>), grid, dim3(256), 0, stream, e);
+  else if (streams_past(c.T, columns))
+    hipLaunchKernelGGL((lora_expand_kernel<true, true>), grid, dim3(256), 0, stream, e);
+  else
+    hipLaunchKernelGGL((lora_expand_kernel<true, false>), grid, dim3(256), 0, stream, e);
   return hip_status(hipGetLastError(), "adapter kernels' launch");
 }
 
@@ -1018,41 +1245,52 @@ mbq_status launch_lora_backward(const LoraCall& c, hipStream_t stream) {
     wy = wy && wide(c.dY[p], c.N[p], 4, 16);
     w = w && wide(c.B[p], c.N[p], 8, 16);
   }
+  char* const ws = c.ws + plan.partial;
+  FragmentArgs f = {};
+  f.t = s.t;
+  f.n = c.n;
+  f.steps = (c.r + 31) / 32;
+  f.g_fragments = c.dA[0] ? reinterpret_cast<uint4*>(ws) : nullptr;
+  f.h_fragments = c.dB[0] ? reinterpret_cast<uint4*>(ws + plan.fragments) : nullptr;
+  f.by_token = c.dX ? reinterpret_cast<uint4*>(ws + 2 * plan.fragments) : nullptr;
+  for (int p = 0; p < c.n; ++p) f.h[p] = c.Hin[p];
   if (c.dX || c.dA[0]) {
     if (w && wy)
       shrink<float, true>(s, c.n, stream);
     else
       shrink<float, false>(s, c.n, stream);
   }
+  if (c.dX || c.dA[0] || c.dB[0])
+    hipLaunchKernelGGL(lora_fragment_kernel, dim3(s.t.tiles, c.n, 2 * f.steps), dim3(64), 0, stream, f);
+  GradientArgs g = {};
+  bool wx = true;
+  int64_t dx_blocks = 0;
   if (c.dX) {
-    ExpandArgs e = {};
+    ExpandArgs& e = g.dx;
     e.t = s.t;
     e.sources = c.n;
+    e.steps = f.steps;
+    e.by_token = f.by_token;
     for (int p = 0; p < c.n; ++p) e.w[p] = c.A[p];
     e.base[0] = c.dx_base;
     e.y[0] = c.dX;
     e.L[0] = c.K;
-    expand(e, 1, wide(c.dX, c.K, 4, 16) && wide(c.dx_base, c.K, 4, 16), stream);
+    dx_blocks = expand_blocks(&e, 1);
+    wx = wide(c.dX, c.K, 4, 16) && wide(c.dx_base, c.K, 4, 16);
   }
-  char* ws = c.ws + plan.partial;
   JoinArgs join = {};
   join.T = (int)c.T;
   join.offsets = c.offsets;
   bool joins = false;
+  int64_t join_blocks = 1;
+  char* more = ws + 2 * plan.fragments + plan.by_token;
   for (int side = 0; side < 2; ++side) {  // dA from g and X, dB from h and dY
-    char* const fragments = ws;
-    ws += plan.fragments;
-    if (!(side ? c.dB[0] : c.dA[0])) continue;
-    FragmentArgs f = {};
-    f.t = s.t;
-    f.fragments = reinterpret_cast<uint4*>(fragments);
-    for (int p = 0; p < c.n; ++p) f.h[p] = side ? c.Hin[p] : nullptr;
-    hipLaunchKernelGGL(lora_fragment_kernel, dim3(s.t.tiles, c.n, s.t.rt), dim3(64), 0, stream, f);
-    OuterArgs o = {};
+    OuterArgs& o = side ? g.y : g.x;
     o.t = s.t;
-    o.fragments = f.fragments;
+    o.fragments = side ? f.h_fragments : f.g_fragments;
     o.chunk = side ? plan.chunk_y : plan.chunk_x;
-    o.groups = (s.t.rt + 3) / 4;
+    o.chunks = (int)(c.T / o.chunk + c.adapters + 1);
+    o.groups = outer_groups(s.t.rt, side ? kUnitsY : kUnitsX);
     int64_t most = 0;
     for (int p = 0; p < c.n; ++p) {
       o.x[p] = side ? (const void*)c.dY[p] : c.X;
@@ -1060,28 +1298,34 @@ mbq_status launch_lora_backward(const LoraCall& c, hipStream_t stream) {
       o.d[p] = side ? c.dB[p] : c.dA[p];
       most = o.L[p] > most ? o.L[p] : most;
       if (c.T > o.chunk) {
-        char* const more = c.ws + plan.partial + 2 * plan.fragments + (side && c.T > plan.chunk_x ? c.n * plan.more_x : 0);
-        size_t at = 0;
-        for (int i = 0; i < p; ++i) at += side ? plan.more_y[i] : plan.more_x;
-        o.more[p] = reinterpret_cast<float*>(more + at);
         const int k = side * MBQ_MAX_GROUP + p;
+        o.more[p] = reinterpret_cast<float*>(more);
+        more += side ? plan.more_y[p] : plan.more_x;
+        if (!o.d[p]) continue;
         join.chunk[k] = o.chunk;
         join.d[k] = o.d[p];
         join.more[k] = o.more[p];
         join.values[k] = (int64_t)c.r * o.L[p];
         joins = true;
+        const int64_t blocks = up(join.values[k], 1024) / 1024;
+        if (blocks > join_blocks) join_blocks = blocks < 1024 ? blocks : 1024;
       }
     }
+    if (!o.d[0]) continue;
     o.blocks = (int)blocks_of(most, side ? kWidthY : kWidthX);
-    if (!side)
-      outer<uint16_t, true>(o, c.n, stream);
-    else if (wy)
-      outer<float, true>(o, c.n, stream);
-    else
-      outer<float, false>(o, c.n, stream);
+    o.round = (int)xcd_blocks((int64_t)o.chunks * o.blocks);
+    (side ? g.y_blocks : g.x_blocks) = o.round * o.groups * c.n;
   }
+  const unsigned blocks = (unsigned)(g.y_blocks + g.x_blocks + dx_blocks);
+  if (blocks == 0) return MBQ_OK;
+  if (s.t.rt == 1)
+    gradients<1>(g, wy, wx, streams_past(c.T, c.K), blocks, stream);
+  else if (s.t.rt == 2)
+    gradients<2>(g, wy, wx, streams_past(c.T, c.K), blocks, stream);
+  else
+    gradients<4>(g, wy, wx, streams_past(c.T, c.K), blocks, stream);
   if (joins)
-    hipLaunchKernelGGL(lora_join_kernel, dim3((unsigned)c.adapters, 64, 2 * MBQ_MAX_GROUP), dim3(256), 0, stream, join);
+    hipLaunchKernelGGL(lora_join_kernel, dim3((unsigned)c.adapters, (unsigned)join_blocks, 2 * MBQ_MAX_GROUP), dim3(256), 0, stream, join);
   return hip_status(hipGetLastError(), "adapter gradients' launch");
 }
 
