@@ -162,8 +162,8 @@ def load() -> ctypes.CDLL:
     return lib
 
 
-def _stage():
-    """The stage call's native half (csrc/mbq_torch.cpp); nothing else of the binding needs it."""
+def _native_half():
+    """The native half (csrc/mbq_torch.cpp) of the stage calls and of those beside a frozen blob; the others do without it."""
     global _native
     if _native is None:
         lib = load()
@@ -175,8 +175,13 @@ def _stage():
                       ("mbq_routed_linear_group", "mbq_routed_linear_group_cfg", "mbq_route_workspace_bytes",
                        "mbq_linear_workspace_bytes", "mbq_last_error")],
                     MbqError, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
+        native.bind_beside(*[ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in
+                             ("mbq_lora_group", "mbq_lora_workspace_bytes", "mbq_lora_backward_group",
+                              "mbq_lora_backward_workspace_bytes", "mbq_balance_loss_group",
+                              "mbq_balance_loss_workspace_bytes", "mbq_route_backward_group",
+                              "mbq_route_backward_workspace_bytes")])
         _native = native
-    return _native.stage
+    return _native
 
 
 def _check(status: int, what: str) -> None:
@@ -404,7 +409,7 @@ def mbq_routed_linear_group(X: torch.Tensor, Wr: Sequence[torch.Tensor], br: Seq
                             ws_linear: Optional[torch.Tensor] = None, algo: int = ALGO_AUTO):
     """One stage: route X with every router, then the routed outputs.  -> (routing, Y) lists.  Native (csrc/mbq_torch.cpp):
     what is left to the binding is allocated there."""
-    return _stage()(X, Wr, br, blobs, Ns, routing, Y, ws_route, ws_linear, algo, 0)
+    return _native_half().stage(X, Wr, br, blobs, Ns, routing, Y, ws_route, ws_linear, algo, 0)
 
 
 # ---- other slice configurations ----------------------------------------------------------------------
@@ -514,7 +519,7 @@ def mbq_routed_linear_group_cfg(X: torch.Tensor, Wr: Sequence[torch.Tensor], br:
                                 Y: Optional[Sequence[torch.Tensor]] = None, ws_route: Optional[torch.Tensor] = None,
                                 ws_linear: Optional[torch.Tensor] = None, algo: int = ALGO_AUTO):
     """One stage under a slice configuration: route X with every E-output router, then the routed outputs."""
-    return _stage()(X, Wr, br, blobs, Ns, routing, Y, ws_route, ws_linear, algo, ctypes.addressof(cfg))
+    return _native_half().stage(X, Wr, br, blobs, Ns, routing, Y, ws_route, ws_linear, algo, ctypes.addressof(cfg))
 
 
 # ---- measurement and diagnostic entry points (include/mbq_bench.h) ----------------------------------
@@ -625,40 +630,20 @@ def mbq_routed_linear_group_act(X: torch.Tensor, abits: int, let_shift: Optional
 
 # ---- beside a frozen blob: adapters, the routers' training ---------------------------------------------
 
-def _need(device: torch.device, dtype: torch.dtype, shape: Sequence[int], t: torch.Tensor, what: str) -> torch.Tensor:
-    """The tensor, if it is a contiguous one of this type and shape on this device; the call runs on the current device's
-    current stream, so tensors of another one are refused."""
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
-        raise AssertionError(f"{what} must be {dtype} {list(shape)}, got {t.dtype} {list(t.shape)}")
-    if t.device != device:
-        raise MbqError(f"{what} is on {t.device}, X on {device}")
-    if not t.is_cuda or not t.is_contiguous():
-        raise MbqError("tensors handed to libmbq must be contiguous device tensors")
-    return t
-
-
-def _on_current_device(t: torch.Tensor) -> torch.device:
-    if not t.is_cuda:
-        raise MbqError("tensors handed to libmbq must be contiguous device tensors")
-    if t.device.index != torch.cuda.current_device():
-        raise MbqError(f"the tensors are on {t.device}, the current device is {torch.cuda.current_device()}")
-    return t.device
-
-
-def _addresses(tensors: Optional[Sequence[Optional[torch.Tensor]]]):
-    """Host array of device pointers, null for what is None."""
-    return None if tensors is None else (ctypes.c_void_p * len(tensors))(*[None if t is None else t.data_ptr() for t in tensors])
-
-
 def mbq_lora_sort(adapter: torch.Tensor, n_adapters: int, out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None):
     """adapter int32 [T] (a value outside 0 .. n_adapters-1: none) -> (perm int32 [T], offsets int32 [n_adapters + 1])."""
-    dev = _on_current_device(adapter)
-    T = adapter.numel()
-    _need(dev, torch.int32, (T,), adapter, "adapter")
+    if not adapter.is_cuda:
+        raise MbqError("tensors handed to libmbq must be contiguous device tensors")
+    assert adapter.dtype == torch.int32 and adapter.dim() == 1
+    T, dev = adapter.numel(), adapter.device
+    if dev.index != torch.cuda.current_device():
+        raise MbqError(f"the tensors are on {dev}, the current device is {torch.cuda.current_device()}")
     if out is None:
         out = (torch.empty(T, dtype=torch.int32, device=dev), torch.empty(n_adapters + 1, dtype=torch.int32, device=dev))
-    perm = _need(dev, torch.int32, (T,), out[0], "perm")
-    offsets = _need(dev, torch.int32, (n_adapters + 1,), out[1], "offsets")
+    perm, offsets = out
+    assert perm.dtype == offsets.dtype == torch.int32 and perm.shape == (T,) and offsets.shape == (n_adapters + 1,)
+    if perm.device != dev or offsets.device != dev:
+        raise MbqError(f"perm is on {perm.device}, offsets on {offsets.device}, adapter on {dev}")
     _check(load().mbq_lora_sort(_ptr(adapter), T, n_adapters, _ptr(perm), _ptr(offsets), _stream()), "mbq_lora_sort")
     return perm, offsets
 
@@ -673,27 +658,6 @@ def lora_backward_workspace(T: int, K: int, Ns: Sequence[int], n_adapters: int, 
     return torch.empty(max(256, int(n)), dtype=torch.uint8, device=device)
 
 
-def _lora_inputs(X, A, B, tokens, scale, ranks):
-    """What both directions check -> (device, T, K, adapters, r, widths)."""
-    dev = _on_current_device(X)
-    if X.dim() != 2 or len(A) != len(B) or len(A) < 1 or A[0].dim() != 3:
-        raise AssertionError("X must be a matrix, A and B as many pools [adapters, r, columns] as there are projections")
-    T, K = X.shape
-    n, r = A[0].shape[:2]
-    _need(dev, torch.bfloat16, (T, K), X, "X")
-    for a, b in zip(A, B):
-        _need(dev, torch.bfloat16, (n, r, K), a, "A")
-        _need(dev, torch.bfloat16, (n, r, b.shape[-1]), b, "B")
-    adapter, perm, offsets = tokens
-    _need(dev, torch.int32, (T,), adapter, "adapter")
-    _need(dev, torch.int32, (T,), perm, "perm")
-    _need(dev, torch.int32, (n + 1,), offsets, "offsets")
-    _need(dev, torch.float32, (n,), scale, "scale")
-    if ranks is not None:
-        _need(dev, torch.int32, (n,), ranks, "ranks")
-    return dev, T, K, n, r, [int(b.shape[2]) for b in B]
-
-
 def mbq_lora_group(X: torch.Tensor, A: Sequence[torch.Tensor], B: Sequence[torch.Tensor],
                    tokens: Tuple[torch.Tensor, torch.Tensor, torch.Tensor], scale: torch.Tensor,
                    ranks: Optional[torch.Tensor] = None, base: Optional[Sequence[Optional[torch.Tensor]]] = None,
@@ -703,26 +667,9 @@ def mbq_lora_group(X: torch.Tensor, A: Sequence[torch.Tensor], B: Sequence[torch
 
     X bf16 [T, K]; A_p bf16 [adapters, r, K], B_p bf16 [adapters, r, N_p]; tokens = (adapter, *mbq_lora_sort(adapter, n));
     scale fp32 [adapters]; ranks int32 [adapters] or None; base_p fp32 [T, N_p] or None (zero), may be Y_p.
-    H: buffers fp32 [T, r] per projection that the backward pass wants, or None."""
-    dev, T, K, n, r, Ns = _lora_inputs(X, A, B, tokens, scale, ranks)
-    if Y is None:
-        Y = [torch.empty((T, N), dtype=torch.float32, device=dev) for N in Ns]
-    if len(Y) != len(Ns) or (base is not None and len(base) != len(Ns)) or (H is not None and len(H) != len(Ns)):
-        raise AssertionError("one Y, base and H per projection")
-    for i, N in enumerate(Ns):
-        _need(dev, torch.float32, (T, N), Y[i], "Y")
-        if base is not None and base[i] is not None:
-            _need(dev, torch.float32, (T, N), base[i], "base")
-        if H is not None:
-            _need(dev, torch.float32, (T, r), H[i], "H")
-    if ws is None:
-        ws = lora_workspace(T, K, len(Ns), r, dev)
-    widths = (ctypes.c_int64 * len(Ns))(*Ns)
-    _check(load().mbq_lora_group(X.data_ptr(), T, K, len(Ns), _addresses(A), _addresses(B), widths, n, r,
-                                 None if ranks is None else ranks.data_ptr(), scale.data_ptr(), tokens[0].data_ptr(),
-                                 tokens[1].data_ptr(), tokens[2].data_ptr(), _addresses(base), _addresses(Y), _addresses(H),
-                                 _ptr(ws), ws.numel(), _stream()), "mbq_lora_group")
-    return list(Y)
+    H: buffers fp32 [T, r] per projection that the backward pass wants, or None.  Native (csrc/mbq_torch.cpp), as the calls
+    below; tensors of another device than the current one are refused."""
+    return _native_half().lora(X, A, B, tokens, scale, ranks, base, Y, H, ws)
 
 
 def mbq_lora_backward_group(X: torch.Tensor, A: Sequence[torch.Tensor], B: Sequence[torch.Tensor],
@@ -735,46 +682,11 @@ def mbq_lora_backward_group(X: torch.Tensor, A: Sequence[torch.Tensor], B: Seque
 
     dY_p fp32 [T, N_p]; H_p as the forward call left them; base fp32 [T, K] or None: a gradient of X that dX is added to, may
     be dX."""
-    dev, T, K, n, r, Ns = _lora_inputs(X, A, B, tokens, scale, ranks)
-    f32 = dict(dtype=torch.float32, device=dev)
-    if dX is None:
-        dX = torch.empty((T, K), **f32)
-    if dA is None:
-        dA = [torch.empty((n, r, K), **f32) for _ in Ns]
-    if dB is None:
-        dB = [torch.empty((n, r, N), **f32) for N in Ns]
-    if not len(dY) == len(H) == len(dA) == len(dB) == len(Ns):
-        raise AssertionError("one dY, H, dA and dB per projection")
-    _need(dev, torch.float32, (T, K), dX, "dX")
-    if base is not None:
-        _need(dev, torch.float32, (T, K), base, "base")
-    for i, N in enumerate(Ns):
-        _need(dev, torch.float32, (T, N), dY[i], "dY")
-        _need(dev, torch.float32, (T, r), H[i], "H")
-        _need(dev, torch.float32, (n, r, K), dA[i], "dA")
-        _need(dev, torch.float32, (n, r, N), dB[i], "dB")
-    if ws is None:
-        ws = lora_backward_workspace(T, K, Ns, n, r, dev)
-    widths = (ctypes.c_int64 * len(Ns))(*Ns)
-    _check(load().mbq_lora_backward_group(X.data_ptr(), T, K, len(Ns), _addresses(A), _addresses(B), widths, n, r,
-                                          None if ranks is None else ranks.data_ptr(), scale.data_ptr(),
-                                          tokens[0].data_ptr(), tokens[1].data_ptr(), tokens[2].data_ptr(), _addresses(dY),
-                                          _addresses(H), None if base is None else base.data_ptr(), dX.data_ptr(),
-                                          _addresses(dA), _addresses(dB), _ptr(ws), ws.numel(), _stream()),
-           "mbq_lora_backward_group")
-    return dX, list(dA), list(dB)
+    return _native_half().lora_backward(X, A, B, tokens, scale, dY, H, ranks, base, dX, dA, dB, ws)
 
 
 def balance_loss_workspace(T: int, n_proj: int, device) -> torch.Tensor:
     return torch.empty(max(256, int(load().mbq_balance_loss_workspace_bytes(T, n_proj))), dtype=torch.uint8, device=device)
-
-
-def _mask(dev, T: int, mask: Optional[torch.Tensor]) -> Optional[int]:
-    if mask is None:
-        return None
-    if mask.dtype not in (torch.bool, torch.uint8):
-        raise AssertionError("mask must be bool or uint8")
-    return _need(dev, mask.dtype, (T,), mask, "mask").data_ptr()
 
 
 def mbq_balance_loss_group(logits: Sequence[torch.Tensor], coef: float = 1.0, mask: Optional[torch.Tensor] = None,
@@ -784,32 +696,7 @@ def mbq_balance_loss_group(logits: Sequence[torch.Tensor], coef: float = 1.0, ma
 
     mask bool or uint8 [T] (0 leaves a token out) or None; target: P wanted shares, None for equal ones.  dlogits is the
     gradient of the loss (None without want_grad).  out: buffers as returned, to write into."""
-    if len(logits) < 1 or logits[0].dim() != 2:
-        raise AssertionError("logits must be one matrix [T, P] per router")
-    dev = _on_current_device(logits[0])
-    T, P = logits[0].shape
-    for S in logits:
-        _need(dev, torch.float64, (T, P), S, "logits")
-    if target is not None and len(target) != P:
-        raise AssertionError("target must have one share per precision")
-    if out is None:
-        out = [(torch.empty(P, dtype=torch.int32, device=dev), torch.empty(1, dtype=torch.float32, device=dev),
-                torch.empty((T, P), dtype=torch.float32, device=dev) if want_grad else None) for _ in logits]
-    if len(out) != len(logits):
-        raise AssertionError("one (counts, loss, dlogits) per router")
-    for counts, loss, grad in out:
-        _need(dev, torch.int32, (P,), counts, "counts")
-        _need(dev, torch.float32, (1,), loss, "loss")
-        if want_grad:
-            _need(dev, torch.float32, (T, P), grad, "dlogits")
-    if ws is None:
-        ws = balance_loss_workspace(T, len(logits), dev)
-    shares = None if target is None else (ctypes.c_double * P)(*[float(q) for q in target])
-    _check(load().mbq_balance_loss_group(len(logits), _addresses(logits), T, P, _mask(dev, T, mask), shares, float(coef),
-                                         _addresses([o[0] for o in out]), _addresses([o[1] for o in out]),
-                                         _addresses([o[2] for o in out]) if want_grad else None, _ptr(ws), ws.numel(),
-                                         _stream()), "mbq_balance_loss_group")
-    return [tuple(o) for o in out]
+    return _native_half().balance(logits, coef, mask, target, want_grad, out, ws)
 
 
 def route_backward_workspace(T: int, K: int, n_proj: int, P: int, device) -> torch.Tensor:
@@ -823,33 +710,4 @@ def mbq_route_backward_group(X: torch.Tensor, Wr: Sequence[torch.Tensor], dlogit
                              dbr: Optional[Sequence[torch.Tensor]] = None, ws: Optional[torch.Tensor] = None):
     """Logits' gradients fp32 [T, P] of several routers over one X bf16 [T, K] -> (dX fp32 [T, K], [dWr fp32 [P, K]],
     [dbr fp32 [P]]).  mask bool or uint8 [T] or None; base fp32 [T, K] or None: what dX is added to, may be dX."""
-    dev = _on_current_device(X)
-    if X.dim() != 2 or len(Wr) != len(dlogits) or len(Wr) < 1:
-        raise AssertionError("X must be a matrix, dlogits one per router")
-    T, K = X.shape
-    P = Wr[0].shape[0]
-    f32 = dict(dtype=torch.float32, device=dev)
-    _need(dev, torch.bfloat16, (T, K), X, "X")
-    if dX is None:
-        dX = torch.empty((T, K), **f32)
-    if dWr is None:
-        dWr = [torch.empty((P, K), **f32) for _ in Wr]
-    if dbr is None:
-        dbr = [torch.empty((P,), **f32) for _ in Wr]
-    if not len(dWr) == len(dbr) == len(Wr):
-        raise AssertionError("one dWr and dbr per router")
-    _need(dev, torch.float32, (T, K), dX, "dX")
-    if base is not None:
-        _need(dev, torch.float32, (T, K), base, "base")
-    for i in range(len(Wr)):
-        _need(dev, torch.float32, (P, K), Wr[i], "Wr")
-        _need(dev, torch.float32, (T, P), dlogits[i], "dlogits")
-        _need(dev, torch.float32, (P, K), dWr[i], "dWr")
-        _need(dev, torch.float32, (P,), dbr[i], "dbr")
-    if ws is None:
-        ws = route_backward_workspace(T, K, len(Wr), P, dev)
-    _check(load().mbq_route_backward_group(X.data_ptr(), T, K, len(Wr), _addresses(Wr), P, _addresses(dlogits),
-                                           _mask(dev, T, mask), None if base is None else base.data_ptr(), dX.data_ptr(),
-                                           _addresses(dWr), _addresses(dbr), _ptr(ws), ws.numel(), _stream()),
-           "mbq_route_backward_group")
-    return dX, list(dWr), list(dbr)
+    return _native_half().route_backward(X, Wr, dlogits, mask, base, dX, dWr, dbr, ws)
