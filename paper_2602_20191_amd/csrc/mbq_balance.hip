@@ -386,12 +386,13 @@ __global__ __launch_bounds__(256) void route_join_kernel(const RouteBackwardArgs
 }
 
 namespace {
-// Tokens of a workgroup: about 1024 workgroups, but at least 64 tokens each, so that the chunks' sums stay small beside X.
+// Tokens of a workgroup: about 1024 workgroups, but at least 32 tokens each, so that the chunks' sums stay small beside X
+// (333 tokens of 2176 columns 12.5 us at 64, 9.7 at 32 and at 16).
 int route_chunk(int64_t T, int64_t K) {
   const int64_t blocks = (K + kRouteColumns - 1) / kRouteColumns;
   int64_t chunk = T * blocks / 1024;
   chunk = (chunk + 15) / 16 * 16;
-  return (int)(chunk < 64 ? 64 : chunk);
+  return (int)(chunk < 32 ? 32 : chunk);
 }
 int64_t route_chunks(int64_t T, int64_t K) { return (T + route_chunk(T, K) - 1) / route_chunk(T, K); }
 

@@ -154,9 +154,9 @@ struct DecodeArgs {
   float* partial;  // [projection][token][part][r]
 };
 
-// Part of h[t][.]: grid (parts of K, tokens, projections), four rows of A at a time per wavefront.
+// Part of h[t][.]: grid (parts of K x 16 ranks, tokens, projections), four rows of A a wavefront.
 __global__ __launch_bounds__(256) void lora_decode_shrink_kernel(const DecodeArgs d) {
-  const int part = blockIdx.x, t = blockIdx.y, p = blockIdx.z, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int block = blockIdx.x / d.parts, part = blockIdx.x - block * d.parts, t = blockIdx.y, p = blockIdx.z, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int a = d.adapter[t];
   if ((unsigned)a >= (unsigned)d.n) return;
   const int own = own_rank(d.ranks, a, d.r);
@@ -164,7 +164,8 @@ __global__ __launch_bounds__(256) void lora_decode_shrink_kernel(const DecodeArg
   const uint16_t* x = d.X + (int64_t)t * d.K;
   const uint16_t* w = d.A[p] + (int64_t)a * d.r * d.K;
   float* out = d.partial + ((int64_t)(p * d.T + t) * d.parts + part) * d.r;
-  for (int j0 = wave; j0 < own; j0 += 16) {
+  const int j0 = 16 * block + wave;
+  if (j0 < own) {
     float s[4] = {0.f, 0.f, 0.f, 0.f};
     for (int k = begin + lane * 8; k < end; k += kDecodeColumns) {
       const uint4 xv = *reinterpret_cast<const uint4*>(x + k);
@@ -194,71 +195,217 @@ __global__ __launch_bounds__(256) void lora_decode_shrink_kernel(const DecodeArg
   }
 }
 
-// y[t][.] = base + scale sum_j h[j] B[j][.]: one wavefront per 512 columns of a token; 16 rows of B are on their way while h
-// is put together.  kWide: eight neighbouring columns a lane; else columns 64 apart, one value at a time.
+// y[t][.] = base + scale sum_j h[j] B[j][.] for 512 columns of a token: four wavefronts take rows of B in turn, up to 16 each
+// on their way while h is put together, and are added in LDS.  kWide: eight neighbouring columns a lane; else columns 64
+// apart, one value at a time.
 template <bool kWide>
-__global__ __launch_bounds__(64) void lora_decode_expand_kernel(const DecodeArgs d) {
-  constexpr int kAhead = 16;
+__global__ __launch_bounds__(256) void lora_decode_expand_kernel(const DecodeArgs d) {
+  constexpr int kAhead = kWide ? 16 : 4, kRow = kDecodeColumns + 4;
   __shared__ float h[MBQ_LORA_MAX_RANK];
-  const int t = blockIdx.y, p = blockIdx.z, lane = threadIdx.x;
-  const int64_t N = d.N[p];
-  const int64_t c0 = (int64_t)blockIdx.x * kDecodeColumns + (kWide ? lane * 8 : lane);
-  if ((int64_t)blockIdx.x * kDecodeColumns >= N) return;
-  const int a = d.adapter[t];
+  __shared__ __align__(16) float sums[4][kRow];
+  const int t = blockIdx.y, p = blockIdx.z, tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int64_t N = d.N[p], first = (int64_t)blockIdx.x * kDecodeColumns;
+  if (first >= N) return;
+  const int a = __builtin_amdgcn_readfirstlane(d.adapter[t]);
+  // the two columns that the thread writes
+  const int64_t c1 = first + 2 * tid;
+  float y[2] = {0.f, 0.f};
+  if (d.base[p]) {
+    const float* base = d.base[p] + (int64_t)t * N;
+    if constexpr (kWide) {
+      if (c1 < N) {
+        const float2 v = *reinterpret_cast<const float2*>(base + c1);
+        y[0] = v.x, y[1] = v.y;
+      }
+    } else {
+      if (c1 < N) y[0] = base[c1];
+      if (c1 + 1 < N) y[1] = base[c1 + 1];
+    }
+  }
   const int own = (unsigned)a < (unsigned)d.n ? own_rank(d.ranks, a, d.r) : 0;
   const uint16_t* w = d.B[p] + (own ? (int64_t)a * d.r * N : 0);
-  float w8[kAhead][8];
-  const auto rows = [&](int j0) {
+  const int64_t c0 = first + (kWide ? lane * 8 : lane);
+  uint4 wv[kAhead];
+  const auto load = [&](int j0) {
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
-      const uint16_t* row = w + (int64_t)min(j0 + i, own - 1) * N;
+      if (j0 + 4 * i >= own) break;
+      const uint16_t* row = w + (int64_t)(j0 + 4 * i) * N;
       if constexpr (kWide) {
-        const uint4 v = *reinterpret_cast<const uint4*>(row + min(c0, N - 8));
-        const uint32_t vs[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) w8[i][2 * e] = low_bf16(vs[e]), w8[i][2 * e + 1] = high_bf16(vs[e]);
+        wv[i] = *reinterpret_cast<const uint4*>(row + min(c0, N - 8));
       } else {
+        uint32_t v[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) w8[i][e] = bf16_value(row[min(c0 + 64 * e, N - 1)]);
+        for (int e = 0; e < 8; ++e) v[e] = row[min(c0 + 64 * e, N - 1)];
+        wv[i] = uint4{v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16};
       }
     }
   };
-  if (own) rows(0);
+  load(wave);
   const float* part = d.partial + (int64_t)(p * d.T + t) * d.parts * d.r;
   const float scale = own ? d.scale[a] : 0.f;
-  for (int j = lane; j < d.r; j += 64) {
+  for (int j = tid; j < d.r; j += 256) {
     float sum = 0.f;
     if (j < own)
-      for (int s = 0; s < d.parts; ++s) sum += part[s * d.r + j];
+      for (int s = 0; s < d.parts; s += 8) {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = s + i < d.parts ? part[(s + i) * d.r + j] : 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += v[i];
+      }
     if (d.H[p] && blockIdx.x == 0) d.H[p][(int64_t)t * d.r + j] = sum;
     h[j] = sum * scale;
   }
   __syncthreads();
   float acc[8] = {};
+  for (int j0 = wave; j0 < own; j0 += 4 * kAhead) {
+    if (j0 > wave) load(j0);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      if (j0 + 4 * i >= own) break;
+      const float hj = h[j0 + 4 * i];
+      const uint32_t vs[4] = {wv[i].x, wv[i].y, wv[i].z, wv[i].w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[2 * e] += hj * low_bf16(vs[e]), acc[2 * e + 1] += hj * high_bf16(vs[e]);
+    }
+  }
+  if constexpr (kWide) {
+    *reinterpret_cast<float4*>(&sums[wave][8 * lane]) = float4{acc[0], acc[1], acc[2], acc[3]};
+    *reinterpret_cast<float4*>(&sums[wave][8 * lane + 4]) = float4{acc[4], acc[5], acc[6], acc[7]};
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sums[wave][lane + 64 * e] = acc[e];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < 2; ++e) y[e] += (sums[0][2 * tid + e] + sums[1][2 * tid + e]) + (sums[2][2 * tid + e] + sums[3][2 * tid + e]);
+  float* to = d.Y[p] + (int64_t)t * N;
+  if constexpr (kWide) {
+    if (c1 < N) *reinterpret_cast<float2*>(to + c1) = float2{y[0], y[1]};
+  } else {
+    if (c1 < N) to[c1] = y[0];
+    if (c1 + 1 < N) to[c1 + 1] = y[1];
+  }
+}
+
+// Both in one launch, where that costs few bytes: a workgroup forms all of a token's h and the columns of its own.  Every
+// workgroup of a token reads its rows of A, the others' from the caches, but a dependent launch (about 4 us) is saved.
+constexpr int kFusedThreads = 512, kFusedColumns = 4 * kFusedThreads;
+constexpr int kFusedPieces = 8, kFusedPass = kFusedPieces * kDecodeColumns;  // columns of K whose loads are under way together
+template <bool kWide>
+__global__ __launch_bounds__(kFusedThreads) void lora_decode_fused_kernel(const DecodeArgs d) {
+  constexpr int kWaves = kFusedThreads / 64, kAhead = 16;
+  __shared__ float h[MBQ_LORA_MAX_RANK];
+  const int t = blockIdx.y, p = blockIdx.z, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t N = d.N[p];
+  if ((int64_t)blockIdx.x * kFusedColumns >= N) return;
+  const int64_t c0 = (int64_t)blockIdx.x * kFusedColumns + (kWide ? 4 * tid : tid);
+  const auto column = [&](int c) { return c0 + (kWide ? c : kFusedThreads * c); };
+  const int a = d.adapter[t];
+  const uint16_t* x = d.X + (int64_t)t * d.K;
+  uint4 xv[kFusedPieces];
+  const auto load_x = [&](int64_t k0) {
+#pragma unroll
+    for (int i = 0; i < kFusedPieces; ++i) {
+      const int64_t k = k0 + i * kDecodeColumns + lane * 8;
+      xv[i] = uint4{0, 0, 0, 0};
+      if (k < d.K) xv[i] = *reinterpret_cast<const uint4*>(x + k);
+    }
+  };
+  load_x(0);
+  floatx4 y = {0.f, 0.f, 0.f, 0.f};
+  if (d.base[p]) {
+    const float* base = d.base[p] + (int64_t)t * N;
+    if constexpr (kWide) {
+      if (c0 < N) y = *reinterpret_cast<const floatx4*>(base + c0);
+    } else {
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        if (column(c) < N) y[c] = base[column(c)];
+    }
+  }
+  const bool some = (unsigned)a < (unsigned)d.n;
+  const int own = some ? own_rank(d.ranks, a, d.r) : 0;
+  const float scale = some ? d.scale[a] : 0.f;
+  const uint16_t* w = d.B[p] + (some ? (int64_t)a * d.r * N : 0);
+  uint2 wv[kAhead];
+  const auto load_w = [&](int j0) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const uint16_t* row = w + (int64_t)min(j0 + i, own - 1) * N;
+      if constexpr (kWide) {
+        wv[i] = *reinterpret_cast<const uint2*>(row + min(c0, N - 4));
+      } else {
+        wv[i].x = row[min(column(0), N - 1)] | (uint32_t)row[min(column(1), N - 1)] << 16;
+        wv[i].y = row[min(column(2), N - 1)] | (uint32_t)row[min(column(3), N - 1)] << 16;
+      }
+    }
+  };
+  if (own) load_w(0);
+  if (own < d.r && d.H[p] && blockIdx.x == 0)
+    for (int j = own + tid; j < d.r; j += kFusedThreads) d.H[p][(int64_t)t * d.r + j] = 0.f;
+  for (int j0 = 2 * wave; j0 < own; j0 += 2 * kWaves) {
+    const uint16_t* rows = d.A[p] + ((int64_t)a * d.r + j0) * d.K;
+    const int64_t next = j0 + 1 < own ? d.K : 0;
+    float s[2] = {0.f, 0.f};
+    for (int64_t k0 = 0; k0 < d.K; k0 += kFusedPass) {
+      if (d.K > kFusedPass) load_x(k0);
+      uint4 r[2][kFusedPieces];
+#pragma unroll
+      for (int i = 0; i < kFusedPieces; ++i) {
+        const int64_t k = min(k0 + i * kDecodeColumns + lane * 8, d.K - 8);  // (x is zero behind the last column)
+        r[0][i] = *reinterpret_cast<const uint4*>(rows + k);
+        r[1][i] = *reinterpret_cast<const uint4*>(rows + next + k);
+      }
+#pragma unroll
+      for (int i = 0; i < kFusedPieces; ++i) {
+        const bool there = k0 + i * kDecodeColumns + lane * 8 < d.K;
+        const uint32_t xs[4] = {xv[i].x, xv[i].y, xv[i].z, xv[i].w};
+#pragma unroll
+        for (int o = 0; o < 2; ++o) {
+          const uint32_t ws[4] = {r[o][i].x, r[o][i].y, r[o][i].z, r[o][i].w};
+          float sum = 0.f;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            sum += low_bf16(xs[e]) * low_bf16(ws[e]);
+            sum += high_bf16(xs[e]) * high_bf16(ws[e]);
+          }
+          s[o] += there ? sum : 0.f;
+        }
+      }
+    }
+    const bool upper = lane & 32;
+    float sum = (upper ? s[1] : s[0]) + __shfl_xor(upper ? s[0] : s[1], 32, 64);
+#pragma unroll
+    for (int off = 16; off >= 1; off >>= 1) sum += __shfl_xor(sum, off, 64);
+    const int j = j0 + (upper ? 1 : 0);
+    if ((lane & 31) == 0 && j < own) {
+      if (d.H[p] && blockIdx.x == 0) d.H[p][(int64_t)t * d.r + j] = sum;
+      h[j] = sum * scale;
+    }
+  }
+  __syncthreads();
+  floatx4 acc = {0.f, 0.f, 0.f, 0.f};
   for (int j0 = 0; j0 < own; j0 += kAhead) {
-    if (j0) rows(j0);
+    if (j0) load_w(j0);
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       const float hj = j0 + i < own ? h[j0 + i] : 0.f;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) acc[e] += hj * w8[i][e];
+      acc[0] += hj * low_bf16(wv[i].x), acc[1] += hj * high_bf16(wv[i].x);
+      acc[2] += hj * low_bf16(wv[i].y), acc[3] += hj * high_bf16(wv[i].y);
     }
   }
-  const float* base = d.base[p] ? d.base[p] + (int64_t)t * N : nullptr;
-  float* y = d.Y[p] + (int64_t)t * N;
+#pragma unroll
+  for (int c = 0; c < 4; ++c) y[c] += acc[c];
+  float* to = d.Y[p] + (int64_t)t * N;
   if constexpr (kWide) {
-    if (c0 < N) {
-      float4 v[2] = {};
-      if (base) v[0] = *reinterpret_cast<const float4*>(base + c0), v[1] = *reinterpret_cast<const float4*>(base + c0 + 4);
-      v[0].x += acc[0], v[0].y += acc[1], v[0].z += acc[2], v[0].w += acc[3];
-      v[1].x += acc[4], v[1].y += acc[5], v[1].z += acc[6], v[1].w += acc[7];
-      *reinterpret_cast<float4*>(y + c0) = v[0];
-      *reinterpret_cast<float4*>(y + c0 + 4) = v[1];
-    }
+    if (c0 < N) *reinterpret_cast<floatx4*>(to + c0) = y;
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (c0 + 64 * e < N) y[c0 + 64 * e] = (base ? base[c0 + 64 * e] : 0.f) + acc[e];
+    for (int c = 0; c < 4; ++c)
+      if (column(c) < N) to[column(c)] = y[c];
   }
 }
 
@@ -468,6 +615,20 @@ __device__ __forceinline__ void store4(float* p, floatx4 v) {
     *reinterpret_cast<floatx4*>(p) = v;
 }
 
+// Four columns of eight rows, as loaded, into four operands of eight rows each.
+__device__ __forceinline__ void turn(const uint2 v[8], uint4 w[4]) {
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    uint32_t d[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t even = c < 2 ? v[2 * e].x : v[2 * e].y, odd = c < 2 ? v[2 * e + 1].x : v[2 * e + 1].y;
+      d[e] = __builtin_amdgcn_perm(odd, even, c & 1 ? 0x07060302u : 0x05040100u);
+    }
+    w[c] = uint4{d[0], d[1], d[2], d[3]};
+  }
+}
+
 constexpr int kExpandColumns = 256;  // of a workgroup
 struct ExpandArgs {
   TileArgs t;
@@ -476,13 +637,10 @@ struct ExpandArgs {
   float *y[MBQ_MAX_GROUP], *H[MBQ_MAX_GROUP];
   int64_t L[MBQ_MAX_GROUP];
   int outputs, first[MBQ_MAX_GROUP], blocks;  // blocks of columns: an output's first, of all of them
-  int sources;  // projections that add to one output: 1 (forward: the output's own), or all (backward, one output)
-  int steps;    // of 32 ranks of a projection, in by_token
-  const uint4* by_token;
+  bool wide[MBQ_MAX_GROUP];
 };
 
-// y = base + sum over the sources of scale h w for a tile.  h goes 32 ranks at a time (lane: token, eight ranks): cut into
-// pieces through LDS, or (kCut) as lora_fragment_kernel left it; w is turned in registers: a lane loads four columns of eight ranks and pairs ranks up by one byte
+// y = base + scale h w for a tile.  h goes 32 ranks at a time, cut into pieces, through LDS (lane: token, eight ranks); w is turned in registers: a lane loads four columns of eight ranks and pairs ranks up by one byte
 // permutation a dword.  kWide: MFMA c of a set of four yields columns 4 (lane mod 16) + c, so that a lane's four results of
 // one token are one 16-byte access to base and y; else columns 16 c + lane mod 16.  base, and the next step's h and w, are on
 // their way while a step is multiplied.  Bound by reading base and writing y.
@@ -490,7 +648,13 @@ constexpr int kStep = 32, kStride = kStep + 8;
 struct ExpandLds {
   uint16_t pieces[2][3][kTile][kStride];
 };
-template <bool kWide, bool kStream, bool kCut>
+__device__ __forceinline__ int expand_output(const ExpandArgs& s, int block_id) {
+  const int item = xcd_item(block_id, s.t.tiles * s.blocks), block = item - item / s.blocks * s.blocks;
+  int out = 0;
+  while (out + 1 < s.outputs && block >= s.first[out + 1]) ++out;
+  return out;
+}
+template <bool kWide, bool kStream>
 __device__ __forceinline__ void expand_block(const ExpandArgs& s, int block_id, ExpandLds* lds) {
   const int item = xcd_item(block_id, s.t.tiles * s.blocks);
   if (item >= s.t.tiles * s.blocks) return;
@@ -543,22 +707,14 @@ __device__ __forceinline__ void expand_block(const ExpandArgs& s, int block_id, 
 #pragma unroll
     for (int c = 0; c < 4; ++c) acc[h][c] = floatx4{0.f, 0.f, 0.f, 0.f};
 
-  // steps of 32 ranks, source by source
-  const int p0 = s.sources == 1 ? out : 0, per = (own + kStep - 1) / kStep, steps = per * s.sources;
+  const int steps = (own + kStep - 1) / kStep;
   float4 hv;
-  uint4 hf[kCut ? 6 : 1];
   uint2 wv[8];  // four columns of ranks 8 q ..
-  const auto load = [&](int p, int j0) {
-    if constexpr (kCut) {
-      const uint4* from = s.by_token + (((int64_t)tile * s.sources + p) * s.steps + j0 / kStep) * 384 + lane;
-#pragma unroll
-      for (int i = 0; i < 6; ++i) hf[i] = from[64 * i];
-    } else {
-      const int j = j0 + 4 * (tid & 7);
-      hv = float4{0.f, 0.f, 0.f, 0.f};
-      if (j < own) hv = whole_h(s.t, p, place, j);
-    }
-    const uint16_t* w = s.w[p] + (int64_t)at.a * s.t.r * L;
+  const uint16_t* w = s.w[out] + (some ? (int64_t)at.a * s.t.r * L : 0);
+  const auto load = [&](int j0) {
+    const int j = j0 + 4 * (tid & 7);
+    hv = float4{0.f, 0.f, 0.f, 0.f};
+    if (j < own) hv = whole_h(s.t, out, place, j);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {  // ranks that are not there meet zeros
       const uint16_t* row = w + (int64_t)min(j0 + 8 * q + e, own - 1) * L;
@@ -570,15 +726,10 @@ __device__ __forceinline__ void expand_block(const ExpandArgs& s, int block_id, 
       }
     }
   };
-  if (steps) load(p0, 0);
-  int p = p0, j0 = 0;
+  if (steps) load(0);
   for (int step = 0; step < steps; ++step) {
-    uint4 a[kCut ? 6 : 1];
-    if constexpr (kCut) {
-#pragma unroll
-      for (int i = 0; i < 6; ++i) a[i] = hf[i];
-    } else {
-      const int j = j0 + 4 * (tid & 7);
+    {
+      const int j = step * kStep + 4 * (tid & 7);
       float v[4] = {hv.x, hv.y, hv.z, hv.w};
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -594,29 +745,14 @@ __device__ __forceinline__ void expand_block(const ExpandArgs& s, int block_id, 
       for (int i = 0; i < 3; ++i) *reinterpret_cast<uint2*>(&lds->pieces[step & 1][i][tid >> 3][4 * (tid & 7)]) = pc[i];
     }
     uint4 w4[4];
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      uint32_t d[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t even = c < 2 ? wv[2 * e].x : wv[2 * e].y, odd = c < 2 ? wv[2 * e + 1].x : wv[2 * e + 1].y;
-        d[e] = __builtin_amdgcn_perm(odd, even, c & 1 ? 0x07060302u : 0x05040100u);
-      }
-      w4[c] = uint4{d[0], d[1], d[2], d[3]};
-    }
-    j0 += kStep;
-    if (j0 >= own) ++p, j0 = 0;
-    if (step + 1 < steps) load(p, j0);
-    if constexpr (!kCut) __syncthreads();  // (the other buffer's readers passed the barrier before: two buffers do)
+    turn(wv, w4);
+    if (step + 1 < steps) load((step + 1) * kStep);
+    __syncthreads();  // (the other buffer's readers passed the barrier before: two buffers do)
 #pragma unroll
     for (int i = 0; i < 3; ++i)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        uint4 av;
-        if constexpr (kCut)
-          av = a[2 * i + h];
-        else
-          av = *reinterpret_cast<const uint4*>(&lds->pieces[step & 1][i][16 * h + (lane & 15)][8 * q]);
+        const uint4 av = *reinterpret_cast<const uint4*>(&lds->pieces[step & 1][i][16 * h + (lane & 15)][8 * q]);
 #pragma unroll
         for (int c = 0; c < 4; ++c) acc[h][c] = bf::mfma(av, w4[c], acc[h][c]);
       }
@@ -624,7 +760,7 @@ __device__ __forceinline__ void expand_block(const ExpandArgs& s, int block_id, 
   if (H)  // ranks that are not there
     for (int e = tid; e < at.count * s.t.r; e += 256) {
       const int j = e % s.t.r;
-      if (j >= per * kStep) H[(int64_t)token_at(s.t.perm, s.t.T, at.begin + e / s.t.r) * s.t.r + j] = 0.f;
+      if (j >= steps * kStep) H[(int64_t)token_at(s.t.perm, s.t.T, at.begin + e / s.t.r) * s.t.r + j] = 0.f;
     }
   if (!copies) return;
 #pragma unroll
@@ -644,16 +780,24 @@ __device__ __forceinline__ void expand_block(const ExpandArgs& s, int block_id, 
     }
 }
 
-template <bool kWide, bool kStream>
+template <bool kStream>
 __global__ __launch_bounds__(256) void lora_expand_kernel(const ExpandArgs s) {
   __shared__ __align__(16) ExpandLds lds;
-  expand_block<kWide, kStream, false>(s, blockIdx.x, &lds);
+  expand_block<true, kStream>(s, blockIdx.x, &lds);
+}
+// where some output's rows are not 16-byte aligned
+__global__ __launch_bounds__(256) void lora_expand_any_kernel(const ExpandArgs s) {
+  __shared__ __align__(16) ExpandLds lds;
+  if (s.wide[expand_output(s, blockIdx.x)])
+    expand_block<true, false>(s, blockIdx.x, &lds);
+  else
+    expand_block<false, false>(s, blockIdx.x, &lds);
 }
 
 // The operands of the gradients' products, cut into pieces and scaled.  By ranks, for the products over tokens:
 // fragments[projection][tile][unit][piece][lane] holds 16 bytes, rank 16 unit + lane mod 16 of tokens 8 (lane / 16) .. + 7 of
 // the tile.  By tokens, for dX: by_token[tile][projection][32 ranks][piece][half][lane], token 16 half + lane mod 16, ranks
-// 8 (lane / 16) .. + 7.  What is not there is zero.  One wavefront per (tile, projection, 32 ranks), of g (summed over its
+// 8 (lane / 16) .. + 7.  What is not there is zero.  One workgroup per (tile, projection, 32 ranks), of g (summed over its
 // parts) and of h as the forward pass left it.
 struct FragmentArgs {
   TileArgs t;
@@ -661,68 +805,64 @@ struct FragmentArgs {
   const float* h[MBQ_MAX_GROUP];
   uint4 *g_fragments, *h_fragments, *by_token;  // null: not wanted
 };
-__global__ __launch_bounds__(64) void lora_fragment_kernel(const FragmentArgs s) {
-  constexpr int kStride = 36;  // floats: 16-byte rows in LDS, spread over the banks
-  __shared__ __align__(16) float v[kTile][kStride];  // [token][rank]
-  const int tile = blockIdx.x, p = blockIdx.y, step = blockIdx.z >> 1, lane = threadIdx.x, q = lane >> 4;
+__global__ __launch_bounds__(256) void lora_fragment_kernel(const FragmentArgs s) {
+  constexpr int kRow = 36;  // floats of a row in LDS: 16-byte aligned, spread over the banks
+  constexpr int kEach = 4;  // tokens of a thread
+  __shared__ __align__(16) float v[kTile][kRow];  // [token][rank]
+  const int tile = blockIdx.x, p = blockIdx.y, step = blockIdx.z >> 1, tid = threadIdx.x, lane = tid & 63, q = lane >> 4;
   const bool of_h = blockIdx.z & 1;
   if (of_h ? !s.h_fragments : !s.g_fragments && !s.by_token) return;
   const Tile at = find_tile(s.t.offsets, s.t.n, s.t.T, tile, kTile);
   if (at.a >= s.t.n || at.count == 0) return;
   const int own = own_rank(s.t.ranks, at.a, s.t.r);
   const float scale = s.t.scale[at.a];
-  // lane: rank j, every other token
-  const int j = 32 * step + (lane & 31);
-  float sum[kTile / 2];
-#pragma unroll
-  for (int e = 0; e < kTile / 2; ++e) sum[e] = 0.f;
+  const int j = 32 * step + (tid & 31), token0 = kEach * (tid >> 5);
+  float sum[kEach] = {};
   if (j < own) {
     if (of_h) {
 #pragma unroll
-      for (int e = 0; e < kTile / 2; ++e) {
-        const int place = at.begin + min(2 * e + (lane >> 5), at.count - 1);
-        sum[e] = s.h[p][(int64_t)token_at(s.t.perm, s.t.T, place) * s.t.r + j];
-      }
+      for (int e = 0; e < kEach; ++e)
+        sum[e] = s.h[p][(int64_t)token_at(s.t.perm, s.t.T, at.begin + min(token0 + e, at.count - 1)) * s.t.r + j];
     } else {
       const float* from = s.t.partial + ((int64_t)(p * s.t.rt + (j >> 4)) * s.t.T + at.begin) * 16 + (j & 15);
-      for (int i = 0; i < 1 << s.t.parts_log2; ++i, from += (int64_t)s.t.units * s.t.T * 16)
+      const int64_t next = (int64_t)s.t.units * s.t.T * 16;
+      const int parts = 1 << s.t.parts_log2;
+      for (int i = 0; i < parts; i += 4) {
+        float part[4][kEach] = {};
 #pragma unroll
-        for (int e = 0; e < kTile / 2; ++e) sum[e] += from[min(2 * e + (lane >> 5), at.count - 1) * 16];
+        for (int k = 0; k < 4; ++k)
+          if (i + k < parts)
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) part[k][e] = from[(i + k) * next + min(token0 + e, at.count - 1) * 16];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+          for (int e = 0; e < kEach; ++e) sum[e] += part[k][e];
+      }
     }
   }
 #pragma unroll
-  for (int e = 0; e < kTile / 2; ++e) {
-    const int token = 2 * e + (lane >> 5);
-    v[token][lane & 31] = j < own && token < at.count ? sum[e] * scale : 0.f;
-  }
+  for (int e = 0; e < kEach; ++e) v[token0 + e][tid & 31] = j < own && token0 + e < at.count ? sum[e] * scale : 0.f;
   __syncthreads();
+  // wavefronts 0 and 1: the units, 2 and 3: the halves of the tokens
   uint4* const fragments = of_h ? s.h_fragments : s.g_fragments;
-  if (fragments)
+  const int w = tid >> 6, half = w & 1, unit = 2 * step + half;
+  if (w < 2 ? !fragments || unit >= s.t.rt : of_h || !s.by_token) return;
+  float x[8];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int unit = 2 * step + u;
-      if (unit >= s.t.rt) continue;
-      float x[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = v[8 * q + e][16 * u + (lane & 15)];
-      const Pieces pc = cut(x);
-      uint4* to = fragments + (((int64_t)p * s.t.tiles + tile) * s.t.rt + unit) * 192 + lane;
-      to[0] = pc.hi;
-      to[64] = pc.mid;
-      to[128] = pc.lo;
-    }
-  if (!of_h && s.by_token)
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      float x[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = v[16 * h + (lane & 15)][8 * q + e];
-      const Pieces pc = cut(x);
-      uint4* to = s.by_token + (((int64_t)tile * s.n + p) * s.steps + step) * 384 + h * 64 + lane;
-      to[0] = pc.lo;
-      to[128] = pc.mid;
-      to[256] = pc.hi;
-    }
+  for (int e = 0; e < 8; ++e) x[e] = w < 2 ? v[8 * q + e][16 * half + (lane & 15)] : v[16 * half + (lane & 15)][8 * q + e];
+  const Pieces pc = cut(x);
+  if (w < 2) {
+    uint4* to = fragments + (((int64_t)p * s.t.tiles + tile) * s.t.rt + unit) * 192 + lane;
+    to[0] = pc.hi;
+    to[64] = pc.mid;
+    to[128] = pc.lo;
+  } else {
+    uint4* to = s.by_token + (((int64_t)tile * s.n + p) * s.steps + step) * 384 + half * 64 + lane;
+    to[0] = pc.lo;
+    to[128] = pc.mid;
+    to[256] = pc.hi;
+  }
 }
 
 struct OuterArgs {
@@ -961,11 +1101,128 @@ __device__ __forceinline__ void outer_y_block(const OuterArgs& s, int block_id, 
   }
 }
 
+// dX = base + sum over the projections of g A for a tile, 256 columns at a time for `span` of them: as lora_expand_kernel, but
+// with g as lora_fragment_kernel left it and the projections' ranks one after the other in the same sums.  The next step's
+// operands are under way across the blocks of columns.
+struct DxArgs {
+  TileArgs t;
+  const uint16_t* w[MBQ_MAX_GROUP];
+  const float* base;
+  float* y;
+  int64_t L;
+  int blocks, span, n, steps;  // blocks of span * 256 columns; projections; steps of 32 ranks of a projection in by_token
+  const uint4* by_token;
+};
+template <bool kWide, bool kStream>
+__device__ __forceinline__ void dx_block(const DxArgs& s, int block_id) {
+  const int item = xcd_item(block_id, s.t.tiles * s.blocks);
+  if (item >= s.t.tiles * s.blocks) return;
+  const int tile = item / s.blocks, block = item - tile * s.blocks;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = lane >> 4;
+  const Tile at = find_tile(s.t.offsets, s.t.n, s.t.T, tile, kTile);
+  if (at.count == 0) return;
+  const bool some = at.a < s.t.n;
+  const int own = some ? own_rank(s.t.ranks, at.a, s.t.r) : 0;
+  if (own == 0 && s.y == s.base) return;
+  const int64_t L = s.L;
+  int64_t to[2][4];  // a lane's four tokens of either half
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      to[h][i] = (int64_t)token_at(s.t.perm, s.t.T, at.begin + min(16 * h + 4 * q + i, at.count - 1)) * L;
+  const auto there = [&](int h, int i) { return 16 * h + 4 * q + i < at.count; };
+  int64_t c0 = (int64_t)block * s.span * kExpandColumns + wave * 64 + (lane & 15) * (kWide ? 4 : 1);  // of the next loads
+  const auto column = [&](int64_t from, int c) { return from + (kWide ? c : 16 * c); };
+  const int blocks = (int)min((int64_t)s.span, (L - (int64_t)block * s.span * kExpandColumns + kExpandColumns - 1) / kExpandColumns);
+  const int per = (own + kStep - 1) / kStep, steps = per * s.n;
+  floatx4 b[2][4], acc[2][4];
+  uint4 hf[6];
+  uint2 wv[8];
+  const auto load_base = [&](int64_t c) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        b[h][i] = floatx4{0.f, 0.f, 0.f, 0.f};
+        if (!s.base || !there(h, i)) continue;
+        if constexpr (kWide) {
+          if (c < L) b[h][i] = load4<kStream>(s.base + to[h][i] + c);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (column(c, e) < L) b[h][i][e] = s.base[to[h][i] + column(c, e)];
+        }
+      }
+  };
+  const auto load = [&](int64_t c, int p, int j0) {
+    const uint4* from = s.by_token + (((int64_t)tile * s.n + p) * s.steps + j0 / kStep) * 384 + lane;
+#pragma unroll
+    for (int i = 0; i < 6; ++i) hf[i] = from[64 * i];
+    const uint16_t* w = s.w[p] + (int64_t)at.a * s.t.r * L;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {  // ranks that are not there meet zeros
+      const uint16_t* row = w + (int64_t)min(j0 + 8 * q + e, own - 1) * L;
+      if constexpr (kWide) {
+        wv[e] = *reinterpret_cast<const uint2*>(row + min(c, L - 4));
+      } else {
+        wv[e].x = row[min(column(c, 0), L - 1)] | (uint32_t)row[min(column(c, 1), L - 1)] << 16;
+        wv[e].y = row[min(column(c, 2), L - 1)] | (uint32_t)row[min(column(c, 3), L - 1)] << 16;
+      }
+    }
+  };
+  int64_t c = c0;  // of the sums
+  load_base(c);
+  if (steps) load(c0, 0, 0);
+  int p = 0, j0 = 0;  // of the next loads
+  for (int k = 0; k < blocks; ++k) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[h][e] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int step = 0; step < steps; ++step) {
+      uint4 a[6], w4[4];
+#pragma unroll
+      for (int i = 0; i < 6; ++i) a[i] = hf[i];
+      turn(wv, w4);
+      j0 += kStep;
+      if (j0 >= own) {
+        j0 = 0;
+        if (++p == s.n) p = 0, c0 += kExpandColumns;
+      }
+      if (step + 1 < steps || k + 1 < blocks) load(c0, p, j0);
+#pragma unroll
+      for (int i = 0; i < 3; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[h][e] = bf::mfma(a[2 * i + h], w4[e], acc[h][e]);
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (!there(h, i)) continue;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) b[h][i][e] += acc[h][e][i];
+        if constexpr (kWide) {
+          if (c < L) store4<kStream>(s.y + to[h][i] + c, b[h][i]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (column(c, e) < L) s.y[to[h][i] + column(c, e)] = b[h][i][e];
+        }
+      }
+    c += kExpandColumns;
+    if (k + 1 < blocks) load_base(c);
+  }
+}
+
 // What comes after g and h are cut: dB, dA and dX in one launch, the longest first.  Each alone leaves much of the chip
 // waiting for its own loads.
 struct GradientArgs {
   OuterArgs y, x;
-  ExpandArgs dx;
+  DxArgs dx;
   int y_blocks, x_blocks;  // workgroups of dB, of dA; the others do dX
 };
 template <int kUnits, bool kWideY, bool kWideX, bool kStream>
@@ -981,7 +1238,7 @@ __global__ __launch_bounds__(256, 2) void lora_gradient_kernel(const GradientArg
   else if (block < s.y_blocks + s.x_blocks)
     outer_x_block<kUnitsX>(s.x, block - s.y_blocks, &lds.x);
   else
-    expand_block<kWideX, kStream, true>(s.dx, block - s.y_blocks - s.x_blocks, nullptr);
+    dx_block<kWideX, kStream>(s.dx, block - s.y_blocks - s.x_blocks);
 }
 
 // d[a] += the chunks behind an adapter's first, in order.
@@ -995,7 +1252,6 @@ struct JoinArgs {
 };
 __global__ __launch_bounds__(256) void lora_join_kernel(const JoinArgs s) {
   const int a = blockIdx.x, k = blockIdx.z, chunk = s.chunk[k];
-  if (chunk == 0) return;
   const int off = clamped(s.offsets[a], s.T), end = clamped(s.offsets[a + 1], s.T);
   const int chunks = end > off ? (end - off - 1) / chunk : 0;  // behind the first
   if (chunks == 0) return;
@@ -1058,6 +1314,14 @@ int decode_parts(int64_t K, int* columns) {
   return (int)((passes + each - 1) / each);
 }
 
+// One launch instead of two where a token's rows of A are at most 128 KB (4096 columns at rank 16: 16 tokens on three
+// projections 8.7 -> 7.5 us, one token 5.9 either way and one launch less for the host; 256 KB: 6.3 -> 7.9 us) and all
+// workgroups together read at most 32 MB of them (25 MB: 10.2 -> 9.9 us; 50 MB: 15.4 -> 17.5).
+bool decode_fuses(int64_t T, int64_t K, int n, int64_t widest, int r) {
+  const int64_t bytes = K * r * 2;
+  return bytes <= 128 << 10 && T * n * (up(widest, kFusedColumns) / kFusedColumns) * bytes <= 32 << 20;
+}
+
 template <typename In, bool kWide>
 void shrink(const ShrinkArgs& s, int sources, hipStream_t stream) {
   const int units = s.shared ? s.t.units : s.t.rt;
@@ -1102,8 +1366,17 @@ int outer_groups(int rt, int units) { return (rt + units - 1) / units; }
 
 // Tokens of a chunk of the gradients' products: about two workgroups a compute unit, but chunks of at least 8 r tokens, whose
 // arrays are then small beside what a chunk reads.
-int outer_chunk(int64_t T, int64_t workgroups, int r) {
-  int64_t chunk = T * workgroups / 512;
+#ifndef VDX
+#define VDX 512
+#endif
+#ifndef VX
+#define VX 512
+#endif
+#ifndef VY
+#define VY 512
+#endif
+int outer_chunk(int64_t T, int64_t workgroups, int64_t wanted, int r) {
+  int64_t chunk = T * workgroups / wanted;
   if (chunk < 8 * r) chunk = 8 * r;
   if (chunk > T) chunk = T;
   return (int)up(chunk < 1 ? 1 : chunk, kTile * kWaves);
@@ -1124,8 +1397,8 @@ BackwardPlan backward_plan(int64_t T, int64_t K, int n, const int64_t* N, int64_
     blocks += blocks_of(N[p], kWidthY);
   }
   b.parts_log2 = shrink_parts_log2(T, most);
-  b.chunk_x = outer_chunk(T, blocks_of(K, kWidthX) * n * outer_groups(rt, kUnitsX), r);
-  b.chunk_y = outer_chunk(T, blocks * outer_groups(rt, kUnitsY), r);
+  b.chunk_x = outer_chunk(T, blocks_of(K, kWidthX) * n * outer_groups(rt, kUnitsX), VX, r);
+  b.chunk_y = outer_chunk(T, blocks * outer_groups(rt, kUnitsY), VY, r);
   const int64_t tiles = T / kTile + adapters + 1;
   b.partial = up((int64_t)partial_bytes(T, rt * n, b.parts_log2), 256);
   b.fragments = (size_t)n * tiles * rt * 3072;
@@ -1172,12 +1445,20 @@ mbq_status launch_lora(const LoraCall& c, hipStream_t stream) {
       most = c.N[p] > most ? c.N[p] : most;
       w = w && wide(c.B[p], c.N[p], 8, 16) && wide(c.Y[p], c.N[p], 4, 16) && wide(c.base[p], c.N[p], 4, 16);
     }
-    hipLaunchKernelGGL(lora_decode_shrink_kernel, dim3(d.parts, d.T, c.n), dim3(256), 0, stream, d);
+    if (decode_fuses(c.T, c.K, c.n, most, c.r)) {
+      const dim3 one((unsigned)(up(most, kFusedColumns) / kFusedColumns), d.T, c.n);
+      if (w)
+        hipLaunchKernelGGL(lora_decode_fused_kernel<true>, one, dim3(kFusedThreads), 0, stream, d);
+      else
+        hipLaunchKernelGGL(lora_decode_fused_kernel<false>, one, dim3(kFusedThreads), 0, stream, d);
+      return hip_status(hipGetLastError(), "adapter kernel's launch");
+    }
+    hipLaunchKernelGGL(lora_decode_shrink_kernel, dim3(d.parts * ((c.r + 15) / 16), d.T, c.n), dim3(256), 0, stream, d);
     const dim3 grid((unsigned)(up(most, kDecodeColumns) / kDecodeColumns), d.T, c.n);
     if (w)
-      hipLaunchKernelGGL(lora_decode_expand_kernel<true>, grid, dim3(64), 0, stream, d);
+      hipLaunchKernelGGL(lora_decode_expand_kernel<true>, grid, dim3(256), 0, stream, d);
     else
-      hipLaunchKernelGGL(lora_decode_expand_kernel<false>, grid, dim3(64), 0, stream, d);
+      hipLaunchKernelGGL(lora_decode_expand_kernel<false>, grid, dim3(256), 0, stream, d);
     return hip_status(hipGetLastError(), "adapter kernels' launch");
   }
   ShrinkArgs s = {};
@@ -1198,20 +1479,20 @@ mbq_status launch_lora(const LoraCall& c, hipStream_t stream) {
     e.y[p] = c.Y[p];
     e.H[p] = c.H[p];
     e.L[p] = c.N[p];
-    w = w && wide(c.B[p], c.N[p], 4, 8) && wide(c.Y[p], c.N[p], 4, 16) && wide(c.base[p], c.N[p], 4, 16);
+    e.wide[p] = wide(c.B[p], c.N[p], 4, 8) && wide(c.Y[p], c.N[p], 4, 16) && wide(c.base[p], c.N[p], 4, 16);
+    w = w && e.wide[p];
   }
   shrink<uint16_t, true>(s, 1, stream);
   e.t = s.t;
-  e.sources = 1;
   const dim3 grid((unsigned)expand_blocks(&e, c.n));
   int64_t columns = 0;
   for (int p = 0; p < c.n; ++p) columns += c.N[p];
   if (!w)
-    hipLaunchKernelGGL((lora_expand_kernel<false, false>), grid, dim3(256), 0, stream, e);
+    hipLaunchKernelGGL(lora_expand_any_kernel, grid, dim3(256), 0, stream, e);
   else if (streams_past(c.T, columns))
-    hipLaunchKernelGGL((lora_expand_kernel<true, true>), grid, dim3(256), 0, stream, e);
+    hipLaunchKernelGGL(lora_expand_kernel<true>, grid, dim3(256), 0, stream, e);
   else
-    hipLaunchKernelGGL((lora_expand_kernel<true, false>), grid, dim3(256), 0, stream, e);
+    hipLaunchKernelGGL(lora_expand_kernel<false>, grid, dim3(256), 0, stream, e);
   return hip_status(hipGetLastError(), "adapter kernels' launch");
 }
 
@@ -1261,27 +1542,31 @@ mbq_status launch_lora_backward(const LoraCall& c, hipStream_t stream) {
       shrink<float, false>(s, c.n, stream);
   }
   if (c.dX || c.dA[0] || c.dB[0])
-    hipLaunchKernelGGL(lora_fragment_kernel, dim3(s.t.tiles, c.n, 2 * f.steps), dim3(64), 0, stream, f);
+    hipLaunchKernelGGL(lora_fragment_kernel, dim3(s.t.tiles, c.n, 2 * f.steps), dim3(256), 0, stream, f);
   GradientArgs g = {};
   bool wx = true;
   int64_t dx_blocks = 0;
   if (c.dX) {
-    ExpandArgs& e = g.dx;
+    DxArgs& e = g.dx;
     e.t = s.t;
-    e.sources = c.n;
+    e.n = c.n;
     e.steps = f.steps;
     e.by_token = f.by_token;
     for (int p = 0; p < c.n; ++p) e.w[p] = c.A[p];
-    e.base[0] = c.dx_base;
-    e.y[0] = c.dX;
-    e.L[0] = c.K;
-    dx_blocks = expand_blocks(&e, 1);
+    e.base = c.dx_base;
+    e.y = c.dX;
+    e.L = c.K;
+    // about VDX workgroups at the tiles that hold tokens
+    int64_t span = up(c.T, kTile) / kTile * blocks_of(c.K, kExpandColumns) / VDX;
+    e.span = (int)(span < 1 ? 1 : span > 8 ? 8 : span);
+    e.blocks = (int)blocks_of(c.K, e.span * kExpandColumns);
+    dx_blocks = xcd_blocks((int64_t)e.t.tiles * e.blocks);
     wx = wide(c.dX, c.K, 4, 16) && wide(c.dx_base, c.K, 4, 16);
   }
   JoinArgs join = {};
   join.T = (int)c.T;
   join.offsets = c.offsets;
-  bool joins = false;
+  int joins = 0;  // outputs that have chunks
   int64_t join_blocks = 1;
   char* more = ws + 2 * plan.fragments + plan.by_token;
   for (int side = 0; side < 2; ++side) {  // dA from g and X, dB from h and dY
@@ -1298,17 +1583,16 @@ mbq_status launch_lora_backward(const LoraCall& c, hipStream_t stream) {
       o.d[p] = side ? c.dB[p] : c.dA[p];
       most = o.L[p] > most ? o.L[p] : most;
       if (c.T > o.chunk) {
-        const int k = side * MBQ_MAX_GROUP + p;
         o.more[p] = reinterpret_cast<float*>(more);
         more += side ? plan.more_y[p] : plan.more_x;
         if (!o.d[p]) continue;
+        const int k = joins++;
         join.chunk[k] = o.chunk;
         join.d[k] = o.d[p];
         join.more[k] = o.more[p];
         join.values[k] = (int64_t)c.r * o.L[p];
-        joins = true;
         const int64_t blocks = up(join.values[k], 1024) / 1024;
-        if (blocks > join_blocks) join_blocks = blocks < 1024 ? blocks : 1024;
+        if (blocks > join_blocks) join_blocks = blocks < 4096 ? blocks : 4096;
       }
     }
     if (!o.d[0]) continue;
@@ -1325,7 +1609,7 @@ mbq_status launch_lora_backward(const LoraCall& c, hipStream_t stream) {
   else
     gradients<4>(g, wy, wx, streams_past(c.T, c.K), blocks, stream);
   if (joins)
-    hipLaunchKernelGGL(lora_join_kernel, dim3((unsigned)c.adapters, (unsigned)join_blocks, 2 * MBQ_MAX_GROUP), dim3(256), 0, stream, join);
+    hipLaunchKernelGGL(lora_join_kernel, dim3((unsigned)c.adapters, (unsigned)join_blocks, joins), dim3(256), 0, stream, join);
   return hip_status(hipGetLastError(), "adapter gradients' launch");
 }
 
