@@ -6,6 +6,7 @@ namespace mbq {
 
 namespace {
 typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef floatx4 floatx4_any __attribute__((aligned(4)));  // base and dX begin at any float
 __device__ __forceinline__ float low_bf16(uint32_t v) { return __uint_as_float(v << 16); }
 __device__ __forceinline__ float high_bf16(uint32_t v) { return __uint_as_float(v & 0xFFFF0000u); }
 }  // namespace
@@ -213,8 +214,8 @@ struct RouteBackwardArgs {
   float* partial_b;
 };
 
-// kRouters: routers of the call.  kWide: columns 4 lane + c, 16-byte accesses; else columns 64 c + lane.
-template <int kRouters, bool kWide, bool kStream>
+// kRouters: routers of the call.
+template <int kRouters, bool kStream>
 __global__ __launch_bounds__(256) void route_backward_kernel(const RouteBackwardArgs s) {
   constexpr int kOut = kRouters * 4;
   __shared__ float red[kRouteWaves][4][4][64];
@@ -222,8 +223,7 @@ __global__ __launch_bounds__(256) void route_backward_kernel(const RouteBackward
   __shared__ uint32_t keeps[kRouteStage];                // all ones, or zero for a token left out
   const RouteBackwardCall& c = s.c;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), P = c.P;
-  const int64_t K = c.K, c0 = (int64_t)blockIdx.x * kRouteColumns + (kWide ? 4 * lane : lane);
-  const auto column = [&](int i) { return c0 + (kWide ? i : 64 * i); };
+  const int64_t K = c.K, c0 = (int64_t)blockIdx.x * kRouteColumns + 4 * lane;
   float w[kOut][4], sum[kOut][4];
 #pragma unroll
   for (int o = 0; o < kOut; ++o)
@@ -231,7 +231,7 @@ __global__ __launch_bounds__(256) void route_backward_kernel(const RouteBackward
     for (int i = 0; i < 4; ++i) {
       sum[o][i] = 0.f;
       w[o][i] = 0.f;
-      if ((o & 3) < P && column(i) < K) w[o][i] = c.Wr[o >> 2][(int64_t)(o & 3) * K + column(i)];
+      if ((o & 3) < P && c0 < K) w[o][i] = c.Wr[o >> 2][(int64_t)(o & 3) * K + c0 + i];  // (K is a multiple of 128)
     }
   const int64_t t0 = (int64_t)blockIdx.y * s.chunk, t1 = min(t0 + s.chunk, c.T);
   float bias = 0.f;  // thread o of the first workgroups: the sum of dlogits of output o
@@ -247,25 +247,14 @@ __global__ __launch_bounds__(256) void route_backward_kernel(const RouteBackward
       const int64_t row = min(t + k, t1 - 1) * K;
       l.x[k] = uint2{0, 0};
       l.y[k] = floatx4{0.f, 0.f, 0.f, 0.f};
-      if constexpr (kWide) {
-        if (c0 < K) {
-          l.x[k] = *reinterpret_cast<const uint2*>(c.X + row + c0);
-          if (with_base) {
-            if constexpr (kStream)
-              l.y[k] = __builtin_nontemporal_load(reinterpret_cast<const floatx4*>(c.base + row + c0));
-            else
-              l.y[k] = *reinterpret_cast<const floatx4*>(c.base + row + c0);
-          }
-        }
-      } else {
-        uint32_t v[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          v[i] = column(i) < K ? c.X[row + column(i)] : 0;
-          if (with_base && column(i) < K) l.y[k][i] = c.base[row + column(i)];
-        }
-        l.x[k] = uint2{v[0] | v[1] << 16, v[2] | v[3] << 16};
-      }
+      if (c0 >= K) continue;
+      l.x[k] = *reinterpret_cast<const uint2*>(c.X + row + c0);
+      if (!with_base) continue;
+      const floatx4_any* from = reinterpret_cast<const floatx4_any*>(c.base + row + c0);
+      if constexpr (kStream)
+        l.y[k] = __builtin_nontemporal_load(from);
+      else
+        l.y[k] = *from;
     }
   };
   const auto use = [&](const Loads& l, int64_t t, int at) {  // at: where the tokens' dlogits lie
@@ -289,20 +278,12 @@ __global__ __launch_bounds__(256) void route_backward_kernel(const RouteBackward
         }
         y[i] += __uint_as_float(__float_as_uint(g) & keep);
       }
-      if (c.dX) {
-        float* to = c.dX + (t + k) * K;
-        if constexpr (kWide) {
-          if (c0 < K) {
-            if constexpr (kStream)
-              __builtin_nontemporal_store(y, reinterpret_cast<floatx4*>(to + c0));
-            else
-              *reinterpret_cast<floatx4*>(to + c0) = y;
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (column(i) < K) to[column(i)] = y[i];
-        }
+      if (c.dX && c0 < K) {
+        floatx4_any* to = reinterpret_cast<floatx4_any*>(c.dX + (t + k) * K + c0);
+        if constexpr (kStream)
+          __builtin_nontemporal_store(y, to);
+        else
+          *to = y;
       }
     }
   };
@@ -342,11 +323,11 @@ __global__ __launch_bounds__(256) void route_backward_kernel(const RouteBackward
       // wavefront e writes output e
       if (wave < P) {
         float* to = s.partial ? s.partial + ((int64_t)blockIdx.y * outputs + p * P + wave) * K : c.dWr[p] + (int64_t)wave * K;
+        floatx4 v;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float v = (red[0][wave][i][lane] + red[1][wave][i][lane]) + (red[2][wave][i][lane] + red[3][wave][i][lane]);
-          if (column(i) < K) to[column(i)] = v;
-        }
+        for (int i = 0; i < 4; ++i)
+          v[i] = (red[0][wave][i][lane] + red[1][wave][i][lane]) + (red[2][wave][i][lane] + red[3][wave][i][lane]);
+        if (c0 < K) *reinterpret_cast<floatx4_any*>(to + c0) = v;
       }
     }
   if (blockIdx.x == 0 && threadIdx.x < kOut && (threadIdx.x & 3) < P && (c.dbr[0] || s.partial)) {
@@ -397,13 +378,11 @@ int route_chunk(int64_t T, int64_t K) {
 int64_t route_chunks(int64_t T, int64_t K) { return (T + route_chunk(T, K) - 1) / route_chunk(T, K); }
 
 template <int kRouters>
-void route_backward(const RouteBackwardArgs& s, bool wide, bool stream_past, dim3 grid, hipStream_t stream) {
-  if (wide && stream_past)
-    hipLaunchKernelGGL((route_backward_kernel<kRouters, true, true>), grid, dim3(256), 0, stream, s);
-  else if (wide)
-    hipLaunchKernelGGL((route_backward_kernel<kRouters, true, false>), grid, dim3(256), 0, stream, s);
+void route_backward(const RouteBackwardArgs& s, bool stream_past, dim3 grid, hipStream_t stream) {
+  if (stream_past)
+    hipLaunchKernelGGL((route_backward_kernel<kRouters, true>), grid, dim3(256), 0, stream, s);
   else
-    hipLaunchKernelGGL((route_backward_kernel<kRouters, false, false>), grid, dim3(256), 0, stream, s);
+    hipLaunchKernelGGL((route_backward_kernel<kRouters, false>), grid, dim3(256), 0, stream, s);
 }
 }  // namespace
 
@@ -433,14 +412,13 @@ mbq_status launch_route_backward(const RouteBackwardCall& c, hipStream_t stream)
     s.partial = reinterpret_cast<float*>(c.ws);
     s.partial_b = s.partial + chunks * c.n * c.P * c.K;
   }
-  const bool wide = ((uintptr_t)c.dX | (uintptr_t)c.base) % 16 == 0;
   const bool stream_past = c.T * c.K * 4 > (32 << 20);  // more than the L2 caches hold: see mbq_lora.hip
   const dim3 grid((unsigned)((c.K + kRouteColumns - 1) / kRouteColumns), (unsigned)chunks);
   switch (c.n) {
-    case 1: route_backward<1>(s, wide, stream_past, grid, stream); break;
-    case 2: route_backward<2>(s, wide, stream_past, grid, stream); break;
-    case 3: route_backward<3>(s, wide, stream_past, grid, stream); break;
-    default: route_backward<4>(s, wide, stream_past, grid, stream); break;
+    case 1: route_backward<1>(s, stream_past, grid, stream); break;
+    case 2: route_backward<2>(s, stream_past, grid, stream); break;
+    case 3: route_backward<3>(s, stream_past, grid, stream); break;
+    default: route_backward<4>(s, stream_past, grid, stream); break;
   }
   if (s.partial) {
     const int64_t values = (int64_t)c.n * c.P * (c.K + 1);

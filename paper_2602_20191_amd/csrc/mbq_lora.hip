@@ -85,6 +85,10 @@ unsigned xcd_blocks(int64_t items) { return (unsigned)((items + 7) / 8 * 8); }
 bool wide(const void* p, int64_t columns, int per, int bytes) {
   return columns % per == 0 && (uintptr_t)p % (size_t)bytes == 0;
 }
+// Accesses of 16 bytes at the alignment of their elements, which the hardware takes (aligned ones cost the same).
+typedef floatx4 floatx4_any __attribute__((aligned(4)));
+typedef uint32_t uint32x4 __attribute__((ext_vector_type(4)));
+typedef uint32x4 uint32x4_any __attribute__((aligned(2)));
 
 }  // namespace
 
@@ -438,8 +442,7 @@ struct ShrinkArgs {
 // block at 4096 tokens.  The 16-byte pieces of a row lie in LDS at their number xor the row's, which spreads both accesses over the
 // banks.  Four wavefronts and `parts` workgroups share the columns; x is read once for up to kUnits units (the projections
 // that share it).  Bound by reading x.
-// kWide: rows are 16-byte aligned; else single columns are loaded, a row of 64 by a wavefront.
-template <typename In, int kUnits, bool kWide>
+template <typename In, int kUnits>
 __global__ __launch_bounds__(256) void lora_shrink_kernel(const ShrinkArgs s) {
   constexpr bool kExact = sizeof(In) == 2;
   constexpr int kPer = 16 / (int)sizeof(In);     // columns of a 16-byte piece of x
@@ -475,49 +478,53 @@ __global__ __launch_bounds__(256) void lora_shrink_kernel(const ShrinkArgs s) {
   const auto x_at = [&](int row, int piece) { return xs + (row * kXPieces + (piece ^ (row & (kXPieces - 1)))) * 16; };
   const auto w_at = [&](int row, int piece) { return ws + (row * kWPieces + (piece ^ (row & (kWPieces - 1)))) * 16; };
 
-  const In* x[kWide ? kXLoads : 1];
-  const uint16_t* w[kWide ? kWLoads : 1];
-  if constexpr (kWide) {
+  const int xc = lane % kXPieces * kPer, wc = lane % kWPieces * 8;  // the lane's columns of a stage
+  const In* x[kXLoads];
+  const uint16_t* w[kWLoads];
 #pragma unroll
-    for (int i = 0; i < kXLoads; ++i) x[i] = x_row(i * kXRows + lane / kXPieces) + lane % kXPieces * kPer;
+  for (int i = 0; i < kXLoads; ++i) x[i] = x_row(i * kXRows + lane / kXPieces) + xc;
 #pragma unroll
-    for (int i = 0; i < kWLoads; ++i) w[i] = w_row(i * kWRows + lane / kWPieces) + lane % kWPieces * 8;
-  }
+  for (int i = 0; i < kWLoads; ++i) w[i] = w_row(i * kWRows + lane / kWPieces) + wc;
   uint4 xv[kXLoads], wv[kWLoads];
   const auto load = [&](int64_t k) {
     if (k + kCols <= L) {
 #pragma unroll
-      for (int i = 0; i < kXLoads; ++i) xv[i] = *reinterpret_cast<const uint4*>(x[i] + k);
-#pragma unroll
-      for (int i = 0; i < kWLoads; ++i) wv[i] = *reinterpret_cast<const uint4*>(w[i] + k);
-    } else {  // the last columns: pieces are there or not as a whole
-#pragma unroll
       for (int i = 0; i < kXLoads; ++i) {
-        xv[i] = uint4{0, 0, 0, 0};
-        if (k + lane % kXPieces * kPer < L) xv[i] = *reinterpret_cast<const uint4*>(x[i] + k);
+        if constexpr (kExact)
+          xv[i] = *reinterpret_cast<const uint4*>(x[i] + k);
+        else
+          xv[i] = __builtin_bit_cast(uint4, *reinterpret_cast<const floatx4_any*>(x[i] + k));
       }
 #pragma unroll
       for (int i = 0; i < kWLoads; ++i) {
-        wv[i] = uint4{0, 0, 0, 0};
-        if (k + lane % kWPieces * 8 < L) wv[i] = *reinterpret_cast<const uint4*>(w[i] + k);
+        if constexpr (kExact)
+          wv[i] = *reinterpret_cast<const uint4*>(w[i] + k);
+        else
+          wv[i] = __builtin_bit_cast(uint4, *reinterpret_cast<const uint32x4_any*>(w[i] + k));
+      }
+    } else {  // the last columns of an L that is no multiple of 64; the branch also keeps the loads ahead of the products: without it
+              // (where the forward's L, a multiple of 128, needs none) they sank behind them and 18.6 us were 37
+#pragma unroll
+      for (int i = 0; i < kXLoads; ++i) {
+        In v[kPer];
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) v[e] = k + xc + e < L ? x[i][k + e] : In(0);
+        xv[i] = __builtin_bit_cast(uint4, v);
+      }
+#pragma unroll
+      for (int i = 0; i < kWLoads; ++i) {
+        uint16_t v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = k + wc + e < L ? w[i][k + e] : uint16_t(0);
+        wv[i] = __builtin_bit_cast(uint4, v);
       }
     }
   };
-  const auto store = [&](int64_t k) {
-    if constexpr (kWide) {
+  const auto store = [&]() {
 #pragma unroll
-      for (int i = 0; i < kXLoads; ++i) *reinterpret_cast<uint4*>(x_at(i * kXRows + lane / kXPieces, lane % kXPieces)) = xv[i];
+    for (int i = 0; i < kXLoads; ++i) *reinterpret_cast<uint4*>(x_at(i * kXRows + lane / kXPieces, lane % kXPieces)) = xv[i];
 #pragma unroll
-      for (int i = 0; i < kWLoads; ++i) *reinterpret_cast<uint4*>(w_at(i * kWRows + lane / kWPieces, lane % kWPieces)) = wv[i];
-    } else {
-      const bool there = k + lane < L;
-#pragma unroll 8
-      for (int row = 0; row < kTile; ++row)
-        reinterpret_cast<In*>(x_at(row, lane / kPer))[lane % kPer] = there ? x_row(row)[k + lane] : In(0);
-#pragma unroll 8
-      for (int row = 0; row < 16 * kUnits; ++row)
-        reinterpret_cast<uint16_t*>(w_at(row, lane / 8))[lane % 8] = there ? w_row(row)[k + lane] : uint16_t(0);
-    }
+    for (int i = 0; i < kWLoads; ++i) *reinterpret_cast<uint4*>(w_at(i * kWRows + lane / kWPieces, lane % kWPieces)) = wv[i];
   };
   floatx4 acc[kUnits][2];
 #pragma unroll
@@ -552,10 +559,10 @@ __global__ __launch_bounds__(256) void lora_shrink_kernel(const ShrinkArgs s) {
   };
   const int share = part * kWaves + wave, first = share * s.share[source] + min(share, s.extra[source]);
   const int64_t k0 = (int64_t)first * kCols, k1 = k0 + (s.share[source] + (share < s.extra[source] ? 1 : 0)) * kCols;
-  if (kWide && k0 < k1) load(k0);
+  if (k0 < k1) load(k0);
   for (int64_t k = k0; k < k1; k += kCols) {
-    store(k);
-    if (kWide && k + kCols < k1) load(k + kCols);
+    store();
+    if (k + kCols < k1) load(k + kCols);
     use();
   }
   __syncthreads();
@@ -1322,20 +1329,19 @@ bool decode_fuses(int64_t T, int64_t K, int n, int64_t widest, int r) {
   return bytes <= 128 << 10 && T * n * (up(widest, kFusedColumns) / kFusedColumns) * bytes <= 32 << 20;
 }
 
-template <typename In, bool kWide>
+template <typename In>
 void shrink(const ShrinkArgs& s, int sources, hipStream_t stream) {
   const int units = s.shared ? s.t.units : s.t.rt;
   const dim3 grid(xcd_blocks((int64_t)s.t.tiles << s.t.parts_log2), sources, (units + 3) / 4);
   if (units == 1)
-    hipLaunchKernelGGL((lora_shrink_kernel<In, 1, kWide>), grid, dim3(256), 0, stream, s);
+    hipLaunchKernelGGL((lora_shrink_kernel<In, 1>), grid, dim3(256), 0, stream, s);
   else if (units == 2)
-    hipLaunchKernelGGL((lora_shrink_kernel<In, 2, kWide>), grid, dim3(256), 0, stream, s);
+    hipLaunchKernelGGL((lora_shrink_kernel<In, 2>), grid, dim3(256), 0, stream, s);
   else if (units == 3)
-    hipLaunchKernelGGL((lora_shrink_kernel<In, 3, kWide>), grid, dim3(256), 0, stream, s);
+    hipLaunchKernelGGL((lora_shrink_kernel<In, 3>), grid, dim3(256), 0, stream, s);
   else
-    hipLaunchKernelGGL((lora_shrink_kernel<In, 4, kWide>), grid, dim3(256), 0, stream, s);
+    hipLaunchKernelGGL((lora_shrink_kernel<In, 4>), grid, dim3(256), 0, stream, s);
 }
-
 // -> workgroups
 int64_t expand_blocks(ExpandArgs* s, int outputs) {
   s->outputs = outputs;
@@ -1366,17 +1372,8 @@ int outer_groups(int rt, int units) { return (rt + units - 1) / units; }
 
 // Tokens of a chunk of the gradients' products: about two workgroups a compute unit, but chunks of at least 8 r tokens, whose
 // arrays are then small beside what a chunk reads.
-#ifndef VDX
-#define VDX 512
-#endif
-#ifndef VX
-#define VX 512
-#endif
-#ifndef VY
-#define VY 512
-#endif
-int outer_chunk(int64_t T, int64_t workgroups, int64_t wanted, int r) {
-  int64_t chunk = T * workgroups / wanted;
+int outer_chunk(int64_t T, int64_t workgroups, int r) {
+  int64_t chunk = T * workgroups / 512;
   if (chunk < 8 * r) chunk = 8 * r;
   if (chunk > T) chunk = T;
   return (int)up(chunk < 1 ? 1 : chunk, kTile * kWaves);
@@ -1397,8 +1394,8 @@ BackwardPlan backward_plan(int64_t T, int64_t K, int n, const int64_t* N, int64_
     blocks += blocks_of(N[p], kWidthY);
   }
   b.parts_log2 = shrink_parts_log2(T, most);
-  b.chunk_x = outer_chunk(T, blocks_of(K, kWidthX) * n * outer_groups(rt, kUnitsX), VX, r);
-  b.chunk_y = outer_chunk(T, blocks * outer_groups(rt, kUnitsY), VY, r);
+  b.chunk_x = outer_chunk(T, blocks_of(K, kWidthX) * n * outer_groups(rt, kUnitsX), r);
+  b.chunk_y = outer_chunk(T, blocks * outer_groups(rt, kUnitsY), r);
   const int64_t tiles = T / kTile + adapters + 1;
   b.partial = up((int64_t)partial_bytes(T, rt * n, b.parts_log2), 256);
   b.fragments = (size_t)n * tiles * rt * 3072;
@@ -1482,7 +1479,7 @@ mbq_status launch_lora(const LoraCall& c, hipStream_t stream) {
     e.wide[p] = wide(c.B[p], c.N[p], 4, 8) && wide(c.Y[p], c.N[p], 4, 16) && wide(c.base[p], c.N[p], 4, 16);
     w = w && e.wide[p];
   }
-  shrink<uint16_t, true>(s, 1, stream);
+  shrink<uint16_t>(s, 1, stream);
   e.t = s.t;
   const dim3 grid((unsigned)expand_blocks(&e, c.n));
   int64_t columns = 0;
@@ -1517,14 +1514,13 @@ mbq_status launch_lora_backward(const LoraCall& c, hipStream_t stream) {
   s.t = tile_args(c);
   s.t.partial = reinterpret_cast<float*>(c.ws);
   s.t.parts_log2 = plan.parts_log2;
-  bool w = true, wy = true;
+  bool wy = true;
   for (int p = 0; p < c.n; ++p) {
     s.x[p] = c.dY[p];
     s.w[p] = c.B[p];
     s.L[p] = c.N[p];
     shrink_shares(&s, p);
     wy = wy && wide(c.dY[p], c.N[p], 4, 16);
-    w = w && wide(c.B[p], c.N[p], 8, 16);
   }
   char* const ws = c.ws + plan.partial;
   FragmentArgs f = {};
@@ -1535,12 +1531,7 @@ mbq_status launch_lora_backward(const LoraCall& c, hipStream_t stream) {
   f.h_fragments = c.dB[0] ? reinterpret_cast<uint4*>(ws + plan.fragments) : nullptr;
   f.by_token = c.dX ? reinterpret_cast<uint4*>(ws + 2 * plan.fragments) : nullptr;
   for (int p = 0; p < c.n; ++p) f.h[p] = c.Hin[p];
-  if (c.dX || c.dA[0]) {
-    if (w && wy)
-      shrink<float, true>(s, c.n, stream);
-    else
-      shrink<float, false>(s, c.n, stream);
-  }
+  if (c.dX || c.dA[0]) shrink<float>(s, c.n, stream);
   if (c.dX || c.dA[0] || c.dB[0])
     hipLaunchKernelGGL(lora_fragment_kernel, dim3(s.t.tiles, c.n, 2 * f.steps), dim3(256), 0, stream, f);
   GradientArgs g = {};
@@ -1556,8 +1547,8 @@ mbq_status launch_lora_backward(const LoraCall& c, hipStream_t stream) {
     e.base = c.dx_base;
     e.y = c.dX;
     e.L = c.K;
-    // about VDX workgroups at the tiles that hold tokens
-    int64_t span = up(c.T, kTile) / kTile * blocks_of(c.K, kExpandColumns) / VDX;
+    // about two workgroups a compute unit at the tiles that hold tokens
+    const int64_t span = up(c.T, kTile) / kTile * blocks_of(c.K, kExpandColumns) / 512;
     e.span = (int)(span < 1 ? 1 : span > 8 ? 8 : span);
     e.blocks = (int)blocks_of(c.K, e.span * kExpandColumns);
     dx_blocks = xcd_blocks((int64_t)e.t.tiles * e.blocks);
