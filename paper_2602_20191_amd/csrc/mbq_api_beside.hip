@@ -120,6 +120,7 @@ mbq_status mbq_lora_group(const uint16_t* X, int64_t T, int64_t K, int n_proj, c
       return MBQ_ERR_INVALID_ARG;
     }
   }
+  if (!lora_fits(c)) return bad(MBQ_ERR_BAD_SHAPE, who, "too many adapters for outputs this wide");
   st = check_workspace(who, ws, ws_bytes, lora_workspace_bytes(T, K, n_proj, r));
   if (st != MBQ_OK) return st;
   c.ws = (char*)ws;
@@ -133,6 +134,7 @@ size_t mbq_lora_backward_workspace_bytes(int64_t T, int64_t K, int n_proj, const
     return 0;
   for (int p = 0; p < n_proj; ++p)
     if (N_host[p] < 1 || N_host[p] > kMost) return 0;
+  if (!lora_backward_fits(T, K, n_proj, N_host, n_adapters, r)) return 0;
   return lora_backward_workspace_bytes(T, K, n_proj, N_host, n_adapters, r);
 }
 
@@ -161,6 +163,8 @@ mbq_status mbq_lora_backward_group(const uint16_t* X, int64_t T, int64_t K, int 
     }
   }
   if (!aligned(base, 4) || !aligned(dX, 4)) return bad(MBQ_ERR_INVALID_ARG, who, "misaligned base or dX");
+  if (!lora_backward_fits(T, K, n_proj, N_host, n_adapters, r))
+    return bad(MBQ_ERR_BAD_SHAPE, who, "too many adapters for gradients this wide");
   st = check_workspace(who, ws, ws_bytes, lora_backward_workspace_bytes(T, K, n_proj, N_host, n_adapters, r));
   if (st != MBQ_OK) return st;
   c.dx_base = base;

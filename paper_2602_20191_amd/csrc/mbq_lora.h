@@ -29,6 +29,9 @@ struct LoraCall {
 
 mbq_status launch_lora_sort(const int32_t* adapter, int64_t T, int64_t n, int32_t* perm, int32_t* offsets,
                             hipStream_t stream);
+// whether the launches' grids can be that large
+bool lora_fits(const LoraCall& c);
+bool lora_backward_fits(int64_t T, int64_t K, int n, const int64_t* N, int64_t adapters, int r);
 size_t lora_workspace_bytes(int64_t T, int64_t K, int n, int r);
 mbq_status launch_lora(const LoraCall& c, hipStream_t stream);
 size_t lora_backward_workspace_bytes(int64_t T, int64_t K, int n, const int64_t* N, int64_t adapters, int r);

@@ -421,10 +421,24 @@ constexpr int kWaves = 4;
 // ranks of a projection (projection-major), place = where perm has the token.
 struct TileArgs {
   int T, n, r, rt, units, parts_log2, tiles;  // rt: units of a projection
-  const int32_t *perm, *offsets, *ranks;
+  const int32_t *adapter, *perm, *offsets, *ranks;  // adapter: null unless tiles are numbered by places
   const float* scale;
   float* partial;
 };
+// In the forward pass, where the pool has more adapters than the call has tokens, the tiles are numbered by the places of
+// their first tokens instead: T numbers, not T / 32 + n + 1 (96 tokens, 2048 x 2048, rank 16 of 2000 adapters: 46.5 -> 11.8 us; 512 tokens on q,
+// k, v of 4096, 1000 adapters: 276 -> 199).
+__device__ __forceinline__ Tile tile_of(const TileArgs& t, int tile) {
+  if (!t.adapter) return find_tile(t.offsets, t.n, t.T, tile, kTile);
+  const unsigned id = (unsigned)t.adapter[token_at(t.perm, t.T, tile)];
+  Tile at;
+  at.a = id < (unsigned)t.n ? (int)id : t.n;
+  const int off = clamped(t.offsets[at.a], t.T), end = at.a < t.n ? clamped(t.offsets[at.a + 1], t.T) : t.T;
+  at.begin = tile;
+  at.first = (tile - off) / kTile;
+  at.count = tile >= off && (tile - off) % kTile == 0 ? clamped(end - tile, kTile) : 0;
+  return at;
+}
 
 struct ShrinkArgs {
   TileArgs t;
@@ -453,13 +467,14 @@ __global__ __launch_bounds__(256) void lora_shrink_kernel(const ShrinkArgs s) {
   __shared__ __align__(16) char lds[kWaves * (kXBytes + kWBytes)];
   static_assert(sizeof(lds) >= kWaves * kUnits * 8 * 64 * 4, "the sums are joined in the same LDS");
   // the tiles of tokens without an adapter come last: where there are many tiles, the others are dealt out evenly
-  const int tiles = s.t.tiles < 64 ? s.t.tiles : clamped(s.t.offsets[s.t.n], s.t.T) / kTile + s.t.n;
+  const int bare = s.t.tiles < 64 ? 0 : clamped(s.t.offsets[s.t.n], s.t.T);
+  const int tiles = s.t.tiles < 64 ? s.t.tiles : s.t.adapter ? bare : bare / kTile + s.t.n;
   const int item = xcd_item(blockIdx.x, tiles << s.t.parts_log2);
   const int tile = item >> s.t.parts_log2, part = item & ((1 << s.t.parts_log2) - 1);
   if (tile >= tiles) return;
   const int source = blockIdx.y, chunk = blockIdx.z;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = lane >> 4;
-  const Tile at = find_tile(s.t.offsets, s.t.n, s.t.T, tile, kTile);
+  const Tile at = tile_of(s.t, tile);
   if (at.a >= s.t.n || at.count == 0) return;
   const int own = own_rank(s.t.ranks, at.a, s.t.r);
   if (own == 0) return;
@@ -671,7 +686,7 @@ __device__ __forceinline__ void expand_block(const ExpandArgs& s, int block_id, 
   block -= s.first[out];
   const int64_t L = s.L[out];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, q = lane >> 4;
-  const Tile at = find_tile(s.t.offsets, s.t.n, s.t.T, tile, kTile);
+  const Tile at = tile_of(s.t, tile);
   if (at.count == 0) return;
   const bool some = at.a < s.t.n;
   const int own = some ? own_rank(s.t.ranks, at.a, s.t.r) : 0;
@@ -911,6 +926,19 @@ __device__ __forceinline__ bool outer_work(const OuterArgs& s, int block_id, Out
   if (own_rank(s.t.ranks, w.at.a, s.t.r) <= 16 * w.unit0) w.at.count = 0;  // zeros
   return true;
 }
+// A gradient without tokens: four columns a thread.
+template <int kUnits, int kWidth>
+__device__ __forceinline__ void outer_zeros(const OuterArgs& s, const OuterWork& w, int64_t L) {
+  const int64_t c = (int64_t)w.block * kWidth + threadIdx.x % (kWidth / 4) * 4;
+  const int end = min(16 * (w.unit0 + w.units), s.t.r);
+  for (int j = 16 * w.unit0 + threadIdx.x / (kWidth / 4); j < end; j += 1024 / kWidth) {
+    float* to = w.d + (int64_t)j * L + c;
+    if (c + 4 <= L)
+      *reinterpret_cast<floatx4_any*>(to) = floatx4{0.f, 0.f, 0.f, 0.f};
+    else
+      for (int e = 0; c + e < L; ++e) to[e] = 0.f;
+  }
+}
 // The tokens of a lane's eight rows of a tile.
 struct Rows {
   int token[8];
@@ -938,6 +966,10 @@ __device__ __forceinline__ void outer_x_block(const OuterArgs& s, int block_id, 
   if (!outer_work<kUnits, kWidth>(s, block_id, w)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t L = s.L[w.p], c = (int64_t)w.block * kWidth + (lane & 15) * 8;  // (K is a multiple of 128)
+  if (w.at.count == 0) {
+    outer_zeros<kUnits, kWidth>(s, w, L);
+    return;
+  }
   const uint16_t* x = static_cast<const uint16_t*>(s.x[w.p]) + c;
   floatx4 acc[kUnits][8];
 #pragma unroll
@@ -1020,6 +1052,10 @@ __device__ __forceinline__ void outer_y_block(const OuterArgs& s, int block_id, 
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, q = lane >> 4;
   const int64_t L = s.L[w.p], c0 = (int64_t)w.block * kWidth + wave * 64 + (lane & 15) * (kWide ? 4 : 1);
   const auto column = [&](int c) { return c0 + (kWide ? c : 16 * c); };
+  if (w.at.count == 0) {
+    outer_zeros<kUnits, kWidth>(s, w, L);
+    return;
+  }
   const float* x = static_cast<const float*>(s.x[w.p]);
   floatx4 acc[kUnits][4];
 #pragma unroll
@@ -1284,6 +1320,8 @@ __global__ __launch_bounds__(256) void lora_join_kernel(const JoinArgs s) {
 namespace {
 
 constexpr int64_t kCacheBytes = 32 << 20;  // the eight L2 caches
+// Workgroups of 256 threads in a launch: fewer than 2^32 threads, some left for rounding up to the eight XCDs.
+constexpr int64_t kMostBlocks = ((int64_t)1 << 24) - 1024;
 
 int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
@@ -1411,6 +1449,24 @@ BackwardPlan backward_plan(int64_t T, int64_t K, int n, const int64_t* N, int64_
 
 }  // namespace
 
+bool lora_fits(const LoraCall& c) {
+  if (c.T <= kDecodeTokens) return true;
+  int64_t blocks = 0;
+  for (int p = 0; p < c.n; ++p) blocks += blocks_of(c.N[p], kExpandColumns);
+  const int64_t tiles = c.T / kTile + c.adapters + 1;
+  return (c.T < tiles ? c.T : tiles) * blocks <= kMostBlocks;
+}
+bool lora_backward_fits(int64_t T, int64_t K, int n, const int64_t* N, int64_t adapters, int r) {
+  if (T == 0) return true;
+  const BackwardPlan b = backward_plan(T, K, n, N, adapters, r);
+  const int rt = (r + 15) / 16;
+  int64_t most = 0;
+  for (int p = 0; p < n; ++p) most = N[p] > most ? N[p] : most;
+  const int64_t y = (T / b.chunk_y + adapters + 1) * blocks_of(most, kWidthY) * outer_groups(rt, kUnitsY) * n;
+  const int64_t x = (T / b.chunk_x + adapters + 1) * blocks_of(K, kWidthX) * outer_groups(rt, kUnitsX) * n;
+  return y + x + (T / kTile + adapters + 1) * blocks_of(K, kExpandColumns) <= kMostBlocks;
+}
+
 size_t lora_workspace_bytes(int64_t T, int64_t K, int n, int r) {
   int columns;
   if (T <= kDecodeTokens) return (size_t)T * n * r * decode_parts(K, &columns) * 4 + 256;
@@ -1460,6 +1516,10 @@ mbq_status launch_lora(const LoraCall& c, hipStream_t stream) {
   }
   ShrinkArgs s = {};
   s.t = tile_args(c);
+  if (c.T < s.t.tiles) {
+    s.t.tiles = (int)c.T;
+    s.t.adapter = c.adapter;
+  }
   s.t.partial = reinterpret_cast<float*>(c.ws);
   s.t.parts_log2 = shrink_parts_log2(c.T, c.K);
   s.shared = true;

@@ -90,6 +90,17 @@ def test_lora_backward(lib):
     assert lib.mbq_lora_backward_workspace_bytes(4, 128, 1, None, 2, 8) == 0
 
 
+def test_launches_that_no_grid_holds(lib):
+    wide = widths(1 << 24)
+    assert lora(lib, T=1 << 20, adapters=65536, N=wide) == SHAPE
+    assert lora(lib, T=1 << 20, adapters=65536, N=widths(4096)) == WORKSPACE  # (the widths decide)
+    assert lora(lib, T=65, adapters=65536, N=wide) == WORKSPACE  # a tile per token at most
+    assert lora_backward(lib, T=64, K=1 << 20, adapters=65536, r=256) == SHAPE
+    assert lora_backward(lib, T=64, adapters=65536, N=wide) == SHAPE
+    assert lib.mbq_lora_backward_workspace_bytes(64, 128, 1, wide, 65536, 8) == 0
+    assert lib.mbq_lora_backward_workspace_bytes(64, 128, 1, widths(4096), 65536, 8) > 0
+
+
 def balance(lib, **change):
     v = dict(n=1, logits=pointers(F), T=4, P=4, mask=None, target=None, coef=1.0, counts=pointers(F), loss=pointers(F),
              dlogits=pointers(F), ws=F, ws_bytes=0)

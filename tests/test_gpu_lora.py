@@ -5,6 +5,8 @@ Tolerances.  Products of bf16 values are exact in fp32 and every other operand i
 of its sums.  A sum of n terms in fp32, in any order, is off by at most (n - 1) u sum |terms| (u = 2^-24) and, as the roundings
 are independent, by about sqrt(n) u sum |terms| at most; a value passes within (4 sqrt(n) + 16) u sum |terms|, an array within
 (sqrt(n) + 8) u of its norm, where sums of sums add up."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -289,6 +291,56 @@ def test_workspace_contents_do_not_matter(mbq):
             assert torch.equal(case.forward(mbq, ws=ws)[0], want[0])
             got = case.backward(mbq, ws=back)
             assert torch.equal(got[0], want_d[0]) and torch.equal(got[1][0], want_d[1][0]) and torch.equal(got[2][0], want_d[2][0])
+
+
+@pytest.mark.parametrize("T,n,ids", [(65, 70, "any"), (100, 300, "any"), (130, 200, "one"), (300, 2000, "few"), (70, 4100, "none")])
+def test_more_adapters_than_tokens(mbq, T, n, ids):
+    """Beyond the sizes of a decode batch, with a pool that most of the call does not touch."""
+    gen = torch.Generator().manual_seed(n)
+    some = {"any": n, "one": 1, "few": 3, "none": 1}[ids]
+    assignment = torch.randint(0, some, (T,), generator=gen) * (n // some) + (n // some - 1)
+    if ids == "none":
+        assignment[:] = -1
+    elif ids != "one":
+        assignment[torch.rand(T, generator=gen) < 0.2] = -1
+    case = Case(T, 256, (136, 33), n, 20, seed=T, ragged=True, assignment=assignment)
+    H = [torch.full((T, 20), float("nan"), device="cuda") for _ in range(2)]
+    case.check_forward(case.forward(mbq, H=H), H)
+    case.check_backward(*case.backward(mbq))
+
+
+@pytest.mark.parametrize("T,K,Ns,n,r", [(3, 4224, (136, 33), 2, 4), (5, 8192, (2056,), 3, 8), (2, 16384, (24, 7), 2, 3),
+                                        (9, 2176, (300, 101), 5, 40), (6, 1024, (512, 264), 4, 100), (1, 20608, (600,), 1, 70)])
+def test_decode_batches_of_long_rows_and_large_ranks(mbq, T, K, Ns, n, r):
+    """One launch whose rows take several passes, and the two launches that larger factors take."""
+    for ragged in (False, True):
+        case = Case(T, K, Ns, n, r, seed=K + r, ragged=ragged)
+        H = [torch.full((T, r), float("nan"), device="cuda") for _ in Ns]
+        case.check_forward(case.forward(mbq, H=H), H)
+
+
+@pytest.mark.parametrize("T", [20, 300])
+@pytest.mark.parametrize("wanted", ["dX", "dA", "dB", "dX dA", "dX dB", "dA dB", ""])
+def test_gradients_that_are_not_wanted(mbq, T, wanted):
+    """Each subset of the gradients through the C interface, the others and what only they read null, has the bits of the full
+    call."""
+    case = Case(T, 384, (136, 40), 3, 24, seed=T, ragged=True)
+    dX, dA, dB = case.backward(mbq)
+    lib, N = mbq.load(), (ctypes.c_int64 * 2)(*case.Ns)
+    at = lambda ts: (ctypes.c_void_p * len(ts))(*(t.data_ptr() for t in ts))  # noqa: E731
+    X, base, tokens, scale, ranks = case.X.cuda(), case.dx_base.cuda(), case.tokens(mbq), case.scale.cuda(), case.ranks.cuda()
+    A, B, dY, H = ([t.cuda() for t in ts] for ts in (case.A, case.B, case.dY, case.H))
+    ws = mbq.lora_backward_workspace(T, 384, case.Ns, 3, 24, "cuda")
+    got = [torch.full_like(dX, 5.0), *(torch.full_like(d, 5.0) for d in dA + dB)]
+    want = [d if name in wanted.split() else torch.full_like(d, 5.0)
+            for d, name in zip([dX, *dA, *dB], ["dX", "dA", "dA", "dB", "dB"])]
+    status = lib.mbq_lora_backward_group(
+        X.data_ptr(), T, 384, 2, at(A), at(B), N, 3, 24, ranks.data_ptr(), scale.data_ptr(), *(t.data_ptr() for t in tokens), at(dY),
+        at(H) if "dB" in wanted else None, base.data_ptr(), got[0].data_ptr() if "dX" in wanted else None,
+        at(got[1:3]) if "dA" in wanted else None, at(got[3:]) if "dB" in wanted else None, ws.data_ptr(), ws.numel(),
+        torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    assert status == 0 and all(torch.equal(a, b) for a, b in zip(got, want))
 
 
 def test_no_tokens(mbq):
