@@ -1408,10 +1408,12 @@ void gradients(const GradientArgs& g, bool wy, bool wx, bool streams, unsigned b
 }
 int outer_groups(int rt, int units) { return (rt + units - 1) / units; }
 
-// Tokens of a chunk of the gradients' products: about two workgroups a compute unit, but chunks of at least 8 r tokens, whose
-// arrays are then small beside what a chunk reads.
-int outer_chunk(int64_t T, int64_t workgroups, int r) {
-  int64_t chunk = T * workgroups / 512;
+// Tokens of a chunk of the gradients' products: about `wanted` workgroups, but chunks of at least 8 r tokens, whose arrays
+// are then small beside what a chunk reads.  dB wants two workgroups a compute unit (one: 4096 tokens to 2 x 11008, rank 32,
+// 204 -> 210 us); dA, which takes a third of its time, one up to rank 32 (q, k, v of 4096, 2048 tokens, rank 16: two 83.5
+// -> one 78.9 us) and two beyond, where each has more to do (the same at rank 64: one 122, two 115 us).
+int outer_chunk(int64_t T, int64_t workgroups, int64_t wanted, int r) {
+  int64_t chunk = T * workgroups / wanted;
   if (chunk < 8 * r) chunk = 8 * r;
   if (chunk > T) chunk = T;
   return (int)up(chunk < 1 ? 1 : chunk, kTile * kWaves);
@@ -1432,8 +1434,8 @@ BackwardPlan backward_plan(int64_t T, int64_t K, int n, const int64_t* N, int64_
     blocks += blocks_of(N[p], kWidthY);
   }
   b.parts_log2 = shrink_parts_log2(T, most);
-  b.chunk_x = outer_chunk(T, blocks_of(K, kWidthX) * n * outer_groups(rt, kUnitsX), r);
-  b.chunk_y = outer_chunk(T, blocks * outer_groups(rt, kUnitsY), r);
+  b.chunk_x = outer_chunk(T, blocks_of(K, kWidthX) * n * outer_groups(rt, kUnitsX), rt <= 2 ? 256 : 512, r);
+  b.chunk_y = outer_chunk(T, blocks * outer_groups(rt, kUnitsY), 512, r);
   const int64_t tiles = T / kTile + adapters + 1;
   b.partial = up((int64_t)partial_bytes(T, rt * n, b.parts_log2), 256);
   b.fragments = (size_t)n * tiles * rt * 3072;
