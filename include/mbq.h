@@ -450,13 +450,19 @@ mbq_status mbq_routed_linear_group_act(const uint16_t* X, int64_t T, int64_t K, 
  *   H[t][j] = sum_k X[t][k] A[a(t)][j][k]
  *   Y[t][n] = base[t][n] + scale[a(t)] sum_j H[t][j] B[a(t)][j][n]
  * with j below the adapter's own rank ranks[a] (r where ranks is NULL; values are clamped to 0 .. r); what the pool holds in
- * rows beyond it is not used, whatever it is.  fp32 accumulate throughout.
+ * rows beyond it is not used, whatever it is.  fp32 accumulate throughout.  An infinity among the values that are used makes
+ * NaN or infinity of what it enters, of nothing else (beyond 64 tokens fp32 operands go through the matrix cores in pieces,
+ * where infinities become NaN).
  *
  * Tokens are handed over as the linear calls have them, but by adapter:
  *   adapter : int32 [T], the token's adapter; a value outside 0 .. n_adapters-1 is none
  *   perm    : int32 [T], token ids grouped by ascending adapter, those of none last (mbq_lora_sort: stable)
  *   offsets : int32 [n_adapters + 1]: the tokens of adapter a are perm[offsets[a] .. offsets[a+1]-1]
  * The three must be mutually consistent.
+ *
+ * n_adapters times the widths is limited by a launch's 2^32 threads (4096 adapters, rank 64, on four projections
+ * of 2^15 by 2^15 fit);
+ * MBQ_ERR_BAD_SHAPE beyond.
  */
 #define MBQ_LORA_MAX_RANK 256
 #define MBQ_LORA_MAX_ADAPTERS 65536

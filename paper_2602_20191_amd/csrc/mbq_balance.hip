@@ -15,7 +15,8 @@ __device__ __forceinline__ float high_bf16(uint32_t v) { return __uint_as_float(
 // Everything is fp64: the gradient is p (u_e - sum_j u_j p_j), a small difference where the mix is near its target.  The
 // gradient needs every token's choice, so there are two passes over the logits, one launch for up to kBalanceSmall tokens (a
 // workgroup per router that keeps its tokens' softmax in registers), two launches beyond, the second re-reading logits that the
-// caches hold.  Bound by launches: 32768 tokens and four routers are 6 MB.
+// caches hold.  Bound by launches: 512 tokens 4.0 us; 32768 tokens and four routers, 6 MB, 4.8 and
+// 5.5 us.
 constexpr int kBalanceSmall = 1024, kSmallThreads = 512, kBalanceThreads = 256, kBalanceBlocks = 128;
 
 struct BalanceSums {
@@ -204,7 +205,7 @@ mbq_status launch_balance_loss(const BalanceCall& c, hipStream_t stream) {
 // sums of dWr, and walks over the tokens of its share, four at a time, whose dlogits come from LDS.  32 multiply-adds a column and token for
 // four routers of four outputs, under half of what the vector units do in the time the memory needs, so it is bound by memory.
 // A workgroup's four wavefronts share 256 columns and take tokens in turn; their sums meet in LDS, the chunks' in a second
-// launch, in order.
+// launch, in order.  4096 tokens of 8192 columns, three routers: 79 us, 336 MB at 4.3 TB/s, and 5 us for the join.
 constexpr int kRouteColumns = 256, kRouteWaves = 4, kRouteAhead = 4, kRouteStage = 64;
 
 struct RouteBackwardArgs {

@@ -1,4 +1,4 @@
-// The stage call of the Python binding in native code: allocates what the caller left to the binding, checks the tensors,
+// The stage call of the Python binding, and the calls beside a frozen blob, in native code: allocates what the caller left to the binding, checks the tensors,
 // hands their addresses to the C ABI.  The same work in Python (six allocations, nine argument arrays, two size queries, the
 // stream's handle) took 22.6 us a call of one 2048 x 2048 linear, twice what its two launches take on the GPU.
 // Nothing is kept from one call for the next.
