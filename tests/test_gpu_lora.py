@@ -343,6 +343,38 @@ def test_gradients_that_are_not_wanted(mbq, T, wanted):
     assert status == 0 and all(torch.equal(a, b) for a, b in zip(got, want))
 
 
+@pytest.mark.parametrize("T", [20, 300])
+@pytest.mark.parametrize("value", [float("inf"), float("nan")])
+def test_what_is_not_finite_stays_with_its_token_and_adapter(mbq, T, value):
+    """One token's activations and one other's gradient: their rows and their adapters' gradients, the rest to the bit."""
+    case = Case(T, 256, (136, 33), 4, 20, seed=T)
+    case.adapter[3], case.adapter[7] = 1, 2
+    H = [torch.empty((T, 20), device="cuda") for _ in range(2)]
+    Y, (dX, dA, dB) = case.forward(mbq, H=H), case.backward(mbq)
+    case.X[3, 200] = value
+    H2 = [torch.empty((T, 20), device="cuda") for _ in range(2)]
+    Y2 = case.forward(mbq, H=H2)
+    others = torch.arange(T) != 3
+    for p in range(2):
+        assert torch.equal(Y2[p][others], Y[p][others]) and torch.equal(H2[p][others], H[p][others])
+        assert not torch.isfinite(Y2[p][3]).any() and not torch.isfinite(H2[p][3]).any()
+    dX2, dA2, dB2 = case.backward(mbq)
+    assert torch.equal(dX2, dX) and all(torch.equal(a, b) for a, b in zip(dB2, dB))
+    for p in range(2):
+        assert torch.equal(dA2[p][[0, 2, 3]], dA[p][[0, 2, 3]]) and not torch.isfinite(dA2[p][1, :, 200]).any()
+        keep = torch.arange(256) != 200
+        assert torch.equal(dA2[p][1][:, keep], dA[p][1][:, keep])
+    case.X[3, 200] = 1.0
+    _, dA, _ = case.backward(mbq)
+    case.dY[0][7, 5] = value
+    dX2, dA2, dB2 = case.backward(mbq)
+    others = torch.arange(T) != 7
+    assert torch.equal(dX2[others], dX[others]) and not torch.isfinite(dX2[7]).any()
+    assert torch.equal(dA2[1], dA[1]) and torch.equal(dB2[1], dB[1])
+    assert torch.equal(dA2[0][[0, 1, 3]], dA[0][[0, 1, 3]]) and torch.equal(dB2[0][[0, 1, 3]], dB[0][[0, 1, 3]])
+    assert not torch.isfinite(dA2[0][2]).any() and not torch.isfinite(dB2[0][2, :, 5]).any()
+
+
 def test_no_tokens(mbq):
     case = Case(0, 128, (24,), 2, 8)
     assert case.forward(mbq)[0].shape == (0, 24)
