@@ -1443,8 +1443,8 @@ BackwardPlan backward_plan(int64_t T, int64_t K, int n, const int64_t* N, int64_
   b.chunk_y = outer_chunk(T, blocks * outer_groups(rt, kUnitsY), 512, r);
   const int64_t tiles = T / kTile + adapters + 1;
   b.partial = up((int64_t)partial_bytes(T, rt * n, b.parts_log2), 256);
-  b.fragments = (size_t)n * tiles * rt * 3072;
-  b.by_token = (size_t)n * tiles * ((r + 31) / 32) * 6144;
+  b.fragments = (size_t)n * tiles * rt * 192 * sizeof(uint4);
+  b.by_token = (size_t)n * tiles * ((r + 31) / 32) * 384 * sizeof(uint4);
   b.more_x = up((int64_t)((T - 1) / b.chunk_x + 1) * r * K * 4, 256);
   b.bytes = b.partial + 2 * b.fragments + b.by_token;
   for (int p = 0; p < n; ++p) {
