@@ -443,6 +443,13 @@ __device__ __forceinline__ Tile tile_of(const TileArgs& t, int tile) {
   return at;
 }
 
+// Between a wavefront's LDS stores and its reads of what other lanes stored, either way round.  The hardware takes a wavefront's
+// LDS accesses in their order, so this is no instruction; it keeps the compiler, which sees one lane's addresses, from changing it.
+__device__ __forceinline__ void wavefront_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 struct ShrinkArgs {
   TileArgs t;
   const void* x[MBQ_MAX_GROUP];  // one for all (forward) or one per projection
@@ -581,8 +588,10 @@ __global__ __launch_bounds__(256) void lora_shrink_kernel(const ShrinkArgs s) {
   if (k0 < k1) load(k0);
   for (int64_t k = k0; k < k1; k += kCols) {
     store();
+    wavefront_order();
     if (k + kCols < k1) load(k + kCols);
     use();
+    wavefront_order();
   }
   __syncthreads();
   float* const red = reinterpret_cast<float*>(lds);  // [wave][value][lane]

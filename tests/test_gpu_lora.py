@@ -521,3 +521,12 @@ def test_beside_the_shared_projections(mbq):
     mbq.mbq_lora_group(X, [a.cuda() for a in case.A], [b.cuda() for b in case.B], case.tokens(mbq), case.scale.cuda(),
                        ranks=case.ranks.cuda(), base=Y, Y=Y)
     case.check_forward(Y)
+
+
+def test_many_stages_of_a_wavefront(mbq):
+    """Enough tiles that a wavefront takes eight and more stages of a row through its part of LDS, the last one not whole."""
+    case = Case(3200, 8192, (24,), 2, 16, seed=6)
+    H = [torch.full((3200, 16), float("nan"), device="cuda")]
+    case.check_forward(case.forward(mbq, H=H), H)
+    case = Case(3200, 128, (8200,), 2, 40, seed=7)
+    case.check_backward(*case.backward(mbq))
