@@ -916,6 +916,7 @@ struct OuterArgs {
 struct OuterWork {
   Tile at;
   int p, unit0, units, block, tile0;  // tile0: the chunk's first tile among all
+  int own;                            // the adapter's rank
   float* d;                           // an adapter's first chunk goes to the gradient itself
 };
 template <int kUnits, int kWidth>
@@ -936,7 +937,8 @@ __device__ __forceinline__ bool outer_work(const OuterArgs& s, int block_id, Out
   w.tile0 = off / kTile + w.at.a + w.at.first * (s.chunk / kTile);
   w.d = w.at.first == 0 ? s.d[w.p] + (int64_t)w.at.a * s.t.r * L
                         : s.more[w.p] + (int64_t)(off / s.chunk + w.at.first) * s.t.r * L;
-  if (own_rank(s.t.ranks, w.at.a, s.t.r) <= 16 * w.unit0) w.at.count = 0;  // zeros
+  w.own = own_rank(s.t.ranks, w.at.a, s.t.r);
+  if (w.own <= 16 * w.unit0) w.at.count = 0;  // zeros
   return true;
 }
 // A gradient without tokens: four columns a thread.
@@ -1042,9 +1044,11 @@ __device__ __forceinline__ void outer_x_block(const OuterArgs& s, int block_id, 
     __syncthreads();
     for (int e = tid; e < 16 * kWidth; e += 256) {
       const int j = e / kWidth, col = e - j * kWidth, value = (col & 7) * 4 + (j & 3), l = (j >> 2) * 16 + (col >> 3);
-      if (u < w.units && 16 * (w.unit0 + u) + j < s.t.r)
-        w.d[(int64_t)(16 * (w.unit0 + u) + j) * L + (int64_t)w.block * kWidth + col] =
-            (red[0][value][l] + red[1][value][l]) + (red[2][value][l] + red[3][value][l]);
+      const int rank = 16 * (w.unit0 + u) + j;
+      if (u < w.units && rank < s.t.r) {  // (beyond the adapter's rank a zero met x, whatever that is)
+        const float sum = (red[0][value][l] + red[1][value][l]) + (red[2][value][l] + red[3][value][l]);
+        w.d[(int64_t)rank * L + (int64_t)w.block * kWidth + col] = rank < w.own ? sum : 0.f;
+      }
     }
   }
 }
@@ -1149,10 +1153,11 @@ __device__ __forceinline__ void outer_y_block(const OuterArgs& s, int block_id, 
       const int j = 16 * (w.unit0 + u) + 4 * q + i;
       if (j >= s.t.r) continue;
       float* to = w.d + (int64_t)j * L;
+      const bool used = j < w.own;  // (beyond the adapter's rank a zero met dy, whatever that is)
       const floatx4 value = {acc[u][0][i], acc[u][1][i], acc[u][2][i], acc[u][3][i]};
 #pragma unroll
       for (int c = 0; c < 4; ++c)
-        if (column(c) < L) to[column(c)] = value[c];
+        if (column(c) < L) to[column(c)] = used ? value[c] : 0.f;
     }
   }
 }

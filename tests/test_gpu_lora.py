@@ -530,3 +530,37 @@ def test_many_stages_of_a_wavefront(mbq):
     case.check_forward(case.forward(mbq, H=H), H)
     case = Case(3200, 128, (8200,), 2, 40, seed=7)
     case.check_backward(*case.backward(mbq))
+
+
+@pytest.mark.parametrize("T,r", [(20, 16), (300, 24), (700, 16), (700, 40), (1300, 64)])
+@pytest.mark.parametrize("value", [float("inf"), float("nan")])
+def test_rows_beyond_a_rank_are_zero_whatever_the_values(mbq, T, r, value):
+    """A token of every adapter with values that are not finite, in X and in dY: dA and dB are zero beyond the adapter's rank
+    (in the first chunk of its tokens and in later ones), and the columns that such a value does not enter keep their bits."""
+    own = [r // 2 - 3, r, 0, 1]
+    case = Case(T, 256, (136, 33), 4, r, seed=T + r, assignment=[a % 5 if a % 5 < 4 else -1 for a in range(T)])
+    case.ranks, case.own = torch.tensor(own, dtype=torch.int32), own
+    _, dA, dB = case.backward(mbq)
+    for a in range(4):
+        at = case.tokens_of[a]
+        case.X[at[0], 200], case.X[at[-1], 7] = value, -value
+    keep = torch.ones(256, dtype=torch.bool)
+    keep[[7, 200]] = False
+    _, dA2, dB2 = case.backward(mbq)
+    for p in range(2):
+        assert torch.equal(dB2[p], dB[p]) and torch.equal(dA2[p][:, :, keep], dA[p][:, :, keep])
+        for a in range(4):
+            assert torch.count_nonzero(dA2[p][a, own[a]:]) == 0 and not torch.isfinite(dA2[p][a, :own[a]][:, ~keep]).any()
+    case.X[~torch.isfinite(case.X)] = 1.0
+    for a in range(4):
+        at = case.tokens_of[a]
+        for dY in case.dY:
+            dY[at[0], 5], dY[at[-1], 30] = value, -value
+    _, dA2, dB2 = case.backward(mbq)
+    for p, N in enumerate(case.Ns):
+        keep = torch.ones(N, dtype=torch.bool)
+        keep[[5, 30]] = False
+        assert torch.equal(dB2[p][:, :, keep], dB[p][:, :, keep])
+        for a in range(4):
+            assert torch.count_nonzero(dA2[p][a, own[a]:]) == 0 and torch.count_nonzero(dB2[p][a, own[a]:]) == 0
+            assert not torch.isfinite(dB2[p][a, :own[a]][:, ~keep]).any() and not torch.isfinite(dA2[p][a, :own[a]]).any()
