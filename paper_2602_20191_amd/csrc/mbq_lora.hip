@@ -15,23 +15,30 @@ __device__ __forceinline__ int own_rank(const int32_t* ranks, int a, int r) {
   return own < 0 ? 0 : (own > r ? r : own);
 }
 
-// fp32 operands of the matrix cores.  A value is cut into three bf16 pieces of eight significant bits each, by cutting off
-// and subtracting, both exact: x = hi + mid + lo to the last bit of fp32 (parts below 2^-133 are lost; an infinity comes out
-// as NaN).  Two values make a dword of each piece.
+// fp32 operands of the matrix cores.  A value is cut into three bf16 pieces: the nearest bf16, the nearest to the rest, and
+// what is left, which bf16 holds, as both subtractions are exact: x = hi + mid + lo to the last bit of fp32 (parts below
+// 2^-133 are lost; an infinity comes out as NaN).  mid is at most 2^-8 and lo 2^-17 of the power of two below x, of either
+// sign: cutting off instead leaves 2^-7 and 2^-15 of x's sign, and a product of two values without mid lo and lo mid is then
+// up to 8 x 2^-24 too small, where this is at most 2^-24 off either way.  Values that would round to infinity start with the
+// largest bf16 (and a mid of up to 2^-7).  Two values make a dword of each piece.
 struct Pieces {
   uint4 hi, mid, lo;
 };
 __device__ __forceinline__ uint32_t high_halves(float a, float b) {  // a in the low half
   return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
 }
+__device__ __forceinline__ uint32_t nearest_pair(float a, float b) {
+  typedef float floatx2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(floatx2{a, b}, bf16x2));
+}
 __device__ __forceinline__ void cut_pair(float a, float b, uint32_t& hi, uint32_t& mid, uint32_t& lo) {
-  const float ah = __uint_as_float(__float_as_uint(a) & 0xFFFF0000u), bh = __uint_as_float(__float_as_uint(b) & 0xFFFF0000u);
-  hi = high_halves(ah, bh);
-  a -= ah;
-  b -= bh;
-  const float am = __uint_as_float(__float_as_uint(a) & 0xFFFF0000u), bm = __uint_as_float(__float_as_uint(b) & 0xFFFF0000u);
-  mid = high_halves(am, bm);
-  lo = high_halves(a - am, b - bm);
+  const float most = __uint_as_float(0x7F7F0000u);
+  hi = nearest_pair(__builtin_amdgcn_fmed3f(a, -most, most), __builtin_amdgcn_fmed3f(b, -most, most));
+  a -= low_bf16(hi);
+  b -= high_bf16(hi);
+  mid = nearest_pair(a, b);
+  lo = high_halves(a - low_bf16(mid), b - high_bf16(mid));
 }
 __device__ __forceinline__ Pieces cut(const float v[8]) {
   Pieces p;
@@ -1054,8 +1061,9 @@ __device__ __forceinline__ void outer_x_block(const OuterArgs& s, int block_id, 
 }
 
 // dB[a] = h^T dy over a chunk's tokens, the same way: a lane loads four columns of eight tokens' rows, cuts the values into
-// pieces as it pairs tokens up, and of the nine products of pieces the six above 2^-32 are formed.  256 columns a workgroup,
-// 64 a wavefront, tile after tile; a tile's h is shared through LDS, the next tile's h and dy are under way.
+// pieces as it pairs tokens up.  Of the nine products of pieces six are formed; mid lo, lo mid and lo lo, together at most 2^-24
+// of the product and of either sign, half a step of fp32, are left out.  256 columns a workgroup, 64 a wavefront, tile after
+// tile; a tile's h is shared through LDS, the next tile's h and dy are under way.
 // kWide: columns 4 (lane mod 16) + c, 16-byte accesses; else 16 c + lane mod 16.
 template <int kUnits>
 struct OuterYLds {

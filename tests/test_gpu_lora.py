@@ -564,3 +564,33 @@ def test_rows_beyond_a_rank_are_zero_whatever_the_values(mbq, T, r, value):
         for a in range(4):
             assert torch.count_nonzero(dA2[p][a, own[a]:]) == 0 and torch.count_nonzero(dB2[p][a, own[a]:]) == 0
             assert not torch.isfinite(dB2[p][a, :own[a]][:, ~keep]).any() and not torch.isfinite(dA2[p][a, :own[a]]).any()
+
+
+@pytest.mark.parametrize("r", [16, 40])
+def test_factor_gradients_hold_products_of_all_their_bits(mbq, r):
+    """Adapters of one token each, so that dB is one product h dy per value.  Operands are cut into pieces of eight bits, each
+    the rest rounded to nearest: the second is at most 2^-8 of the power of two below the operand, the third 2^-17.  The products
+    of second and third pieces are left out, 2 x 2^-25 of h dy.  Of the six sums the last is rounded at its full size, to a step
+    2^-23 off if the matrix cores truncate, the others at 2^-7 of it and less, 5 x 2^-30: together under 4 x 2^-24."""
+    T, N = 96, 264
+    gen = torch.Generator().manual_seed(r)
+    awkward = torch.tensor([1 + 2.0 ** -7 - 2.0 ** -23, 1 + 2.0 ** -8 - 2.0 ** -23, 1 + 2.0 ** -8 + 2.0 ** -16 - 2.0 ** -23,
+                            1 + 2.0 ** -8 - 2.0 ** -16 + 2.0 ** -23, 2 - 2.0 ** -23, 1.0])
+
+    def values(*shape):
+        v = torch.where(torch.rand(shape, generator=gen) < 0.5, awkward[torch.randint(0, 6, shape, generator=gen)],
+                        1 + torch.rand(shape, generator=gen))
+        return v * 2.0 ** torch.randint(-30, 31, shape, generator=gen) * (torch.randint(0, 2, shape, generator=gen) * 2 - 1)
+
+    case = Case(T, 128, (N,), T, r, seed=r, assignment=list(range(T)))
+    case.scale[:] = 1.0
+    case.H, case.dY = [values(T, r)], [values(T, N)]
+    largest = torch.finfo(torch.float32).max  # nothing next to it becomes an infinity
+    case.dY[0][:, :3] = torch.tensor([largest, -largest, 2.0 ** 127 * (2 - 2.0 ** -8)])
+    case.H[0][::2] = case.H[0][::2].sign() * 2.0 ** -10 * (1 + torch.rand((T // 2, r), generator=gen))
+    case.H[0][1::2] = case.H[0][1::2].clamp(-0.99, 0.99)
+    _, _, (dB,) = case.backward(mbq)
+    want = case.H[0].double()[:, :, None] * case.dY[0].double()[:, None, :]
+    off = (dB.double().cpu() - want).abs() / want.abs()
+    print(f"[lora] products: worst {float(off.max()) / U:.2f} x 2^-24", flush=True)
+    assert (off <= 4 * U).all()
