@@ -463,6 +463,9 @@ mbq_status mbq_routed_linear_group_act(const uint16_t* X, int64_t T, int64_t K, 
  * n_adapters times the widths is limited by a launch's 2^32 threads (4096 adapters, rank 64, on four projections
  * of 2^15 by 2^15 fit);
  * MBQ_ERR_BAD_SHAPE beyond.
+ *
+ * Workspaces.  The sizes that the queries of this section give do not fall as T grows: one buffer for the longest call serves
+ * the shorter ones with the same other arguments.
  */
 #define MBQ_LORA_MAX_RANK 256
 #define MBQ_LORA_MAX_ADAPTERS 65536

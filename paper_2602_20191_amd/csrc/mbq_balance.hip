@@ -387,8 +387,11 @@ void route_backward(const RouteBackwardArgs& s, bool stream_past, dim3 grid, hip
 }
 }  // namespace
 
+// No call of fewer tokens takes more: T / chunk is at most 33 / 32 of 1024 / blocks, as chunk is at least 32 and at least the
+// whole part of T blocks / 1024.
 size_t route_backward_workspace_bytes(int64_t T, int64_t K, int n, int P) {
-  const int64_t chunks = route_chunks(T, K);
+  const int64_t blocks = (K + kRouteColumns - 1) / kRouteColumns;
+  const int64_t by_length = (T + 31) / 32, by_split = (33 * 32 + blocks - 1) / blocks, chunks = by_length < by_split ? by_length : by_split;
   return chunks > 1 ? (size_t)(chunks * n * P * (K + 1) * 4) + 256 : 256;
 }
 

@@ -1368,10 +1368,11 @@ TileArgs tile_args(const LoraCall& c) {
 }
 // Parts along the columns (their log2): about two workgroups a compute unit at the tiles that hold tokens, and at least a
 // stage of 64 columns per wavefront.
+constexpr int kMostPartsLog2 = 4, kShrinkWorkgroups = 384;
 int shrink_parts_log2(int64_t T, int64_t L) {
   const int64_t tiles = up(T, kTile) / kTile;
   int parts = 0;
-  while (parts < 4 && (tiles << parts) < 384 && (kWaves * 64 << (parts + 1)) <= L) ++parts;
+  while (parts < kMostPartsLog2 && (tiles << parts) < kShrinkWorkgroups && (kWaves * 64 << (parts + 1)) <= L) ++parts;
   return parts;
 }
 void shrink_shares(ShrinkArgs* s, int source) {
@@ -1380,6 +1381,16 @@ void shrink_shares(ShrinkArgs* s, int source) {
   s->extra[source] = (int)(stages % shares);
 }
 size_t partial_bytes(int64_t T, int units, int parts_log2) { return ((size_t)T * units * 64) << parts_log2; }
+// The most of calls of up to T tokens: fewer tokens may have more parts.
+size_t most_partial_bytes(int64_t T, int64_t L, int units) {
+  size_t most = partial_bytes(T, units, shrink_parts_log2(T, L));
+  for (int parts = 1; parts <= kMostPartsLog2; ++parts) {
+    const int64_t last = (int64_t)((kShrinkWorkgroups - 1) >> (parts - 1)) * kTile, t = last < T ? last : T;  // with that many
+    const size_t bytes = partial_bytes(t, units, shrink_parts_log2(t, L));
+    most = bytes > most ? bytes : most;
+  }
+  return most;
+}
 int decode_parts(int64_t K, int* columns) {
   const int64_t passes = up(K, kDecodeColumns) / kDecodeColumns, each = (passes + 15) / 16;
   *columns = (int)(each * kDecodeColumns);
@@ -1439,18 +1450,31 @@ int outer_groups(int rt, int units) { return (rt + units - 1) / units; }
 // are then small beside what a chunk reads.  dB wants two workgroups a compute unit (one: 4096 tokens to 2 x 11008, rank 32,
 // 204 -> 210 us); dA, which takes a third of its time, one up to rank 32 (q, k, v of 4096, 2048 tokens, rank 16: two 83.5
 // -> one 78.9 us) and two beyond, where each has more to do (the same at rank 64: one 122, two 115 us).
-int outer_chunk(int64_t T, int64_t workgroups, int64_t wanted, int r) {
-  int64_t chunk = T * workgroups / wanted;
-  if (chunk < 8 * r) chunk = 8 * r;
+struct OuterSplit {
+  int64_t workgroups, wanted;  // of a chunk; in all
+  int r;
+};
+int outer_chunk(int64_t T, const OuterSplit& s) {
+  int64_t chunk = T * s.workgroups / s.wanted;
+  if (chunk < 8 * s.r) chunk = 8 * s.r;
   if (chunk > T) chunk = T;
   return (int)up(chunk < 1 ? 1 : chunk, kTile * kWaves);
 }
+// The most arrays of chunks of a call of up to T tokens: T / chunk is at most 129 / 128 of wanted / workgroups, as chunk is at
+// least 128 and at least the whole part of T workgroups / wanted.
+int64_t most_chunks(int64_t T, const OuterSplit& s) {
+  const int64_t least = up(8 * s.r, kTile * kWaves);
+  if (T <= least) return 0;
+  const int64_t by_length = up(T, least) / least, by_split = (129 * s.wanted + 128 * s.workgroups - 1) / (128 * s.workgroups);
+  return by_length < by_split ? by_length : by_split;
+}
 int64_t blocks_of(int64_t L, int width) { return up(L, width) / width; }
 
+// most: no call of fewer tokens takes more bytes.
 struct BackwardPlan {
   int parts_log2, chunk_x, chunk_y;
   size_t partial, fragments, by_token, more_x, more_y[MBQ_MAX_GROUP];  // bytes; fragments: of g or of h
-  size_t bytes;
+  size_t most;
 };
 BackwardPlan backward_plan(int64_t T, int64_t K, int n, const int64_t* N, int64_t adapters, int r) {
   BackwardPlan b = {};
@@ -1461,17 +1485,19 @@ BackwardPlan backward_plan(int64_t T, int64_t K, int n, const int64_t* N, int64_
     blocks += blocks_of(N[p], kWidthY);
   }
   b.parts_log2 = shrink_parts_log2(T, most);
-  b.chunk_x = outer_chunk(T, blocks_of(K, kWidthX) * n * outer_groups(rt, kUnitsX), rt <= 2 ? 256 : 512, r);
-  b.chunk_y = outer_chunk(T, blocks * outer_groups(rt, kUnitsY), 512, r);
+  const OuterSplit x = {blocks_of(K, kWidthX) * n * outer_groups(rt, kUnitsX), rt <= 2 ? 256 : 512, r};
+  const OuterSplit y = {blocks * outer_groups(rt, kUnitsY), 512, r};
+  b.chunk_x = outer_chunk(T, x);
+  b.chunk_y = outer_chunk(T, y);
   const int64_t tiles = T / kTile + adapters + 1;
   b.partial = up((int64_t)partial_bytes(T, rt * n, b.parts_log2), 256);
   b.fragments = (size_t)n * tiles * rt * 192 * sizeof(uint4);
   b.by_token = (size_t)n * tiles * ((r + 31) / 32) * 384 * sizeof(uint4);
   b.more_x = up((int64_t)((T - 1) / b.chunk_x + 1) * r * K * 4, 256);
-  b.bytes = b.partial + 2 * b.fragments + b.by_token;
+  b.most = up((int64_t)most_partial_bytes(T, most, rt * n), 256) + 2 * b.fragments + b.by_token;
   for (int p = 0; p < n; ++p) {
     b.more_y[p] = up((int64_t)((T - 1) / b.chunk_y + 1) * r * N[p] * 4, 256);
-    b.bytes += (T > b.chunk_x ? b.more_x : 0) + (T > b.chunk_y ? b.more_y[p] : 0);
+    b.most += up(most_chunks(T, x) * r * K * 4, 256) + up(most_chunks(T, y) * r * N[p] * 4, 256);
   }
   return b;
 }
@@ -1498,8 +1524,9 @@ bool lora_backward_fits(int64_t T, int64_t K, int n, const int64_t* N, int64_t a
 
 size_t lora_workspace_bytes(int64_t T, int64_t K, int n, int r) {
   int columns;
-  if (T <= kDecodeTokens) return (size_t)T * n * r * decode_parts(K, &columns) * 4 + 256;
-  return partial_bytes(T, (r + 15) / 16 * n, shrink_parts_log2(T, K)) + 256;
+  const size_t decode = (size_t)(T < kDecodeTokens ? T : kDecodeTokens) * n * r * decode_parts(K, &columns) * 4;
+  const size_t tiles = T <= kDecodeTokens ? 0 : most_partial_bytes(T, K, (r + 15) / 16 * n);
+  return (decode > tiles ? decode : tiles) + 256;
 }
 
 mbq_status launch_lora(const LoraCall& c, hipStream_t stream) {
@@ -1583,7 +1610,7 @@ mbq_status launch_lora(const LoraCall& c, hipStream_t stream) {
 }
 
 size_t lora_backward_workspace_bytes(int64_t T, int64_t K, int n, const int64_t* N, int64_t adapters, int r) {
-  return T == 0 ? 256 : backward_plan(T, K, n, N, adapters, r).bytes + 256;
+  return T == 0 ? 256 : backward_plan(T, K, n, N, adapters, r).most + 256;
 }
 
 mbq_status launch_lora_backward(const LoraCall& c, hipStream_t stream) {

@@ -185,3 +185,20 @@ def test_binding_refuses_on_the_gpu(mbq):
         mbq.mbq_balance_loss_group([S], target=[0.5, 0.5, 0.0, 0.1])
     with pytest.raises(AssertionError):
         mbq.mbq_route_backward_group(X, [torch.zeros((4, 128), device="cuda")], [torch.zeros((4, 3), device="cuda")])
+
+
+LENGTHS = sorted({*range(0, 700), *range(700, 13000, 16), *range(1, 13000, 31), *(1 << i for i in range(10, 25)), 12256, 12288, 12289})
+
+
+@pytest.mark.parametrize("K,n,r", [(128, 1, 1), (2048, 1, 16), (4096, 3, 16), (4096, 2, 64), (8192, 3, 16), (2176, 2, 20), (28672, 4, 256)])
+def test_a_workspace_serves_shorter_calls(lib, K, n, r):
+    """A buffer that is large enough for T tokens is large enough for fewer."""
+    N = widths(*[K, 1000, K // 4, 3 * K][:n])
+    for of in (lambda T: lib.mbq_lora_workspace_bytes(T, K, n, r),
+               lambda T: lib.mbq_lora_backward_workspace_bytes(T, K, n, N, 4, r),
+               lambda T: lib.mbq_route_backward_workspace_bytes(T, K, n, 1 + r % 4),
+               lambda T: lib.mbq_balance_loss_workspace_bytes(T, n)):
+        sizes = [of(T) for T in LENGTHS]
+        while not sizes[-1]:  # more than a launch holds
+            sizes.pop()
+        assert len(sizes) > 900 and all(sizes) and sizes == sorted(sizes)

@@ -594,3 +594,18 @@ def test_factor_gradients_hold_products_of_all_their_bits(mbq, r):
     off = (dB.double().cpu() - want).abs() / want.abs()
     print(f"[lora] products: worst {float(off.max()) / U:.2f} x 2^-24", flush=True)
     assert (off <= 4 * U).all()
+
+
+def test_one_workspace_for_calls_of_several_lengths(mbq):
+    """Buffers for 2000 tokens serve shorter calls, which stay inside what they ask for themselves."""
+    K, Ns, n, r = 2048, [520, 33], 3, 20
+    large = (mbq.lora_workspace(2000, K, 2, r, "cuda"), mbq.lora_backward_workspace(2000, K, Ns, n, r, "cuda"))
+    for T in (5, 64, 65, 760, 1504, 1505, 2000):
+        case = Case(T, K, Ns, n, r, seed=T)
+        Y, (dX, dA, dB) = case.forward(mbq, ws=large[0]), case.backward(mbq, ws=large[1])
+        own = []
+        for need in (mbq.lora_workspace(T, K, 2, r, "cuda").numel(), mbq.lora_backward_workspace(T, K, Ns, n, r, "cuda").numel()):
+            own.append(torch.full((need + 512,), 7, dtype=torch.uint8, device="cuda"))
+        Y2, (dX2, dA2, dB2) = case.forward(mbq, ws=own[0][:-512]), case.backward(mbq, ws=own[1][:-512])
+        assert all((w[-512:] == 7).all() for w in own)
+        assert torch.equal(dX, dX2) and all(torch.equal(a, b) for a, b in zip(Y + dA + dB, Y2 + dA2 + dB2))
