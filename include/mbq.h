@@ -469,7 +469,8 @@ mbq_status mbq_routed_linear_group_act(const uint16_t* X, int64_t T, int64_t K, 
  */
 #define MBQ_LORA_MAX_RANK 256
 #define MBQ_LORA_MAX_ADAPTERS 65536
-/* perm and offsets of an assignment.  T = 0 is legal (offsets are zero-filled). */
+/* perm and offsets of an assignment.  T = 0 is legal (offsets are zero-filled).  The work grows as T times n_adapters: every
+ * adapter's workgroup reads the whole assignment twice. */
 mbq_status mbq_lora_sort(const int32_t* adapter, int64_t T, int64_t n_adapters, int32_t* perm, int32_t* offsets,
                          void* stream);
 /*
@@ -524,8 +525,9 @@ mbq_status mbq_lora_backward_group(const uint16_t* X, int64_t T, int64_t K, int 
  *   counts[e] = #{t : the choice of t is e},   loss = coef sum_e (counts[e] / n) mean_t(p[t][e]) / target[e]
  *   dlogits[t][e] = d loss / d S[t][e] with the counts as constants
  *                 = coef / n p[t][e] (u_e - sum_j u_j p[t][j]),   u_e = counts[e] / (n target[e])
- * target = 1/P everywhere (NULL) is the usual balance loss P sum_e f_e P_e; with a target mix the sum is least where the
- * mix is met.  Everything is computed in fp64 and rounded once.
+ * target = 1/P everywhere (NULL) is the usual balance loss P sum_e f_e P_e.  The sum is 1 where the counts or the mean
+ * probabilities meet the target mix, and that is the least where the two agree with each other; where they do not (choices near
+ * a tie) it can be less.  Everything is computed in fp64 and rounded once.
  *   logits_host  : HOST array of n_proj fp64 [T][P], 1 <= P <= MBQ_MAX_SLICES, 16-byte aligned for even P
  *   mask         : uint8 [T], 0 leaves the token out, or NULL;   its logits are not used, whatever they are
  *   target_host  : HOST array of P doubles, finite and > 0, or NULL
