@@ -1288,8 +1288,10 @@ __device__ __forceinline__ void dx_block(const DxArgs& s, int block_id) {
 }
 
 // What comes after g and h are cut: dB, dA and dX in one launch, the longest first.  Each alone leaves much of the chip
-// waiting for its own loads.  2048 tokens, 3 x 4096 of 4096, rank 16 44 us (165 MB); 4096 tokens, 2 x 11008, rank 64 146 us: dB's
-// six matrix instructions a pair of operands and the cutting of dY, which two wavefronts a SIMD do not hide behind each other.
+// waiting for its own loads.  2048 tokens, 3 x 4096 of 4096, rank 16 45 us, 183 MB past the L2 caches; 4096 tokens, 2 x 11008,
+// rank 64 146 us, 643 MB at 4.4 TB/s: dY, which g's launch has read already, and X once for each projection and 32 ranks of dA.
+// The vector units are busy 41 % of that time and the matrix units 29 % (dB: six instructions a pair of operands, and cutting dY),
+// and two wavefronts a SIMD do not hide all of it behind the loads.
 struct GradientArgs {
   OuterArgs y, x;
   DxArgs dx;
